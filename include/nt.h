@@ -635,6 +635,119 @@ typedef struct {
 nt_status nt_layernorm_linear_backward(const nt_linear_bwd_args* args, void* stream);
 nt_status nt_layernorm_linear_backward_workspace(const nt_linear_bwd_args* args, uint64_t* bytes);
 
+/* ------------------------------------------------------- window attention
+ * Attention over the packed tokens of each sample with a sliding window, a few
+ * first keys that stay visible, and key/value heads shared by groups of query
+ * heads (Sec. 3.3 "Attention through packed blocks": the output takes the query
+ * structure), of any length, with its gradient.
+ * Sample i has N_i queries (q_layout) and M_i keys and values (kv_layout); its
+ * queries are the last N_i positions of its keys: query t stands at
+ * p = M_i - N_i + t and sees key j, 0 <= j < M_i, where
+ *     j <= p + right             (right = -1: no such bound) and
+ *     j >= p - left or j < sinks (left = -1: no such bound).
+ * left = -1, right = 0 is causal attention, left = right = -1 every key of the
+ * sample.  Query head h reads key/value head h / (heads / kv_heads):
+ *     s_j = scale q[eta_i + t, h] . k[kappa_i + j, h']
+ *     o[eta_i + t, h] = sum_j softmax_j(s)_j v[kappa_i + j, h'],  lse = log sum_j exp(s_j)
+ * over the visible keys.  A query that sees no key gets o = 0, lse = -inf and no
+ * gradient.  Where a wave's 32 queries see only part of a tile of 64 (fp32: 32)
+ * keys, the others of the tile enter with weight 0: their values must be finite.
+ * Keys that no query of a block of 128 / (heads / kv_heads) queries sees, and
+ * keys past kv_lengths, are never read as values and may hold anything.
+ *   Layouts are used for their lengths alone.  Long samples need no pair state:
+ *   nt_from_rect_lengths with every column count 1 describes N_i tokens without
+ *   the N_i^2 cells that would overflow.
+ *   kv_lengths  device int32 [batch] or NULL: the number of keys that sample i
+ *            uses now, of the M_i slots it has (clamped to [0, M_i]); M_i above is
+ *            this number then.  One layout serves a growing cache, and a captured
+ *            graph follows the lengths.  Forward only.
+ *   dtype    bf16 (matrix cores, fp32 softmax and sums) or f32.
+ *   head_dim a multiple of 8, at most 128.
+ *   Row strides are multiples of 8 elements (bf16) or 4 (f32).
+ * Workspace: nt_window_attention_workspace /
+ * nt_window_attention_backward_workspace bytes, 16-byte aligned (they read sizes
+ * and layouts, never the pointers).  Two calls that may run at one time, two
+ * captured graphs among them, need one each.                                  */
+typedef struct {
+  const nt_layout* q_layout;
+  const nt_layout* kv_layout;  /* NULL: q_layout                                  */
+  int32_t heads;               /* query heads, a multiple of kv_heads             */
+  int32_t kv_heads;
+  int32_t head_dim;
+  int32_t left;                /* >= 0, or -1                                     */
+  int32_t right;               /* >= 0, or -1                                     */
+  int32_t sinks;               /* >= 0                                            */
+  float scale;                 /* softmax scale, finite                           */
+  nt_dtype dtype;              /* of q, k, v, o and of dout, dq, dk, dv           */
+  const void* q;               /* [sum N, heads * head_dim]                       */
+  int64_t ld_q;
+  const void* k;               /* [sum M, kv_heads * head_dim]                    */
+  int64_t ld_k;
+  const void* v;
+  int64_t ld_v;
+  void* o;                     /* [sum N, heads * head_dim]; must not alias q, k, v */
+  int64_t ld_o;
+  float* lse;                  /* [heads][ld_lse >= sum N], or NULL (forward: not written) */
+  int64_t ld_lse;
+  const int32_t* kv_lengths;   /* see above                                       */
+  void* workspace;
+  uint64_t workspace_bytes;
+  /* nt_window_attention_backward only (o and lse are the forward's) */
+  const void* dout;            /* gradient of o                                   */
+  int64_t ld_dout;
+  void* dq;                    /* as q, overwritten                               */
+  int64_t ld_dq;
+  void* dk;                    /* as k, overwritten (zero where no query sees a key) */
+  int64_t ld_dk;
+  void* dv;
+  int64_t ld_dv;
+} nt_window_args;
+
+/* Errors: NT_ERR_INVALID_ARG (NULL, sizes, strides, alignment, left or right
+ * below -1, a layout of another device, a missing or too small workspace),
+ * NT_ERR_LAYOUT_MISMATCH (batch sizes differ), NT_ERR_UNSUPPORTED (head_dim),
+ * NT_ERR_OVERFLOW (a sample of 2^30 tokens or more), NT_ERR_HIP.             */
+nt_status nt_window_attention(const nt_window_args* args, void* stream);
+nt_status nt_window_attention_workspace(const nt_window_args* args, uint64_t* bytes);
+
+/* Gradients of nt_window_attention (without kv_lengths):
+ *   P = exp(s - lse), D = sum_c dout o, dS = P (dout v^T - D)
+ *   dq = scale dS k,  dk = scale dS^T q,  dv = P^T dout
+ * summed in fp32 without atomics (the same bits every time), rounded once;
+ * a shared key/value head's gradient is the sum over its query heads.
+ * Errors: as nt_window_attention, and NT_ERR_INVALID_ARG for kv_lengths.     */
+nt_status nt_window_attention_backward(const nt_window_args* args, void* stream);
+nt_status nt_window_attention_backward_workspace(const nt_window_args* args, uint64_t* bytes);
+
+/* ------------------------------------------------------------- embedding
+ * Rows of a table by token id:  y[r] = scale * table[ids[r]], the product in
+ * fp32, rounded once.  An id outside [0, vocab) (padding, say -1) gives a row
+ * of zeros.
+ *   table   [vocab, C] row stride ld_table (table_dtype)
+ *   ids     device, [rows], int32, or int64 with ids_are_64; element-aligned
+ *   y       [rows, C] row stride ld_y (y_dtype, which may differ from the table's)
+ *   C       a multiple of 8
+ * Errors: NT_ERR_INVALID_ARG, NT_ERR_OVERFLOW (rows or vocab beyond int32).  */
+nt_status nt_embedding(const void* table, int64_t vocab, int64_t ld_table, nt_dtype table_dtype, const void* ids,
+                       int32_t ids_are_64, int64_t rows, int32_t C, float scale, void* y, int64_t ld_y,
+                       nt_dtype y_dtype, void* stream);
+
+/* Its gradient with respect to the table:
+ *   dtable[v] (+)= scale * sum over the rows r with ids[r] = v of dy[r]
+ * Rows of the table that no token names are set to zero, or left with
+ * accumulate 1.  fp32 sums, no atomics on them: the tokens are sorted by id
+ * and equal ids added in the order of their rows within fixed chunks, so the
+ * result is the same every time.  ids outside [0, vocab) contribute nothing.
+ *   dy      [rows, C] row stride ld_dy (dtype)
+ *   dtable  [vocab, C] row stride ld_dtable, f32, or bf16 (rounded once per call)
+ * Workspace: nt_embedding_backward_workspace bytes, 16-byte aligned.
+ * Errors: as nt_embedding (also a missing or too small workspace).           */
+nt_status nt_embedding_backward(const void* ids, int32_t ids_are_64, int64_t rows, int64_t vocab, int32_t C,
+                                const void* dy, int64_t ld_dy, nt_dtype dtype, float scale, void* dtable,
+                                int64_t ld_dtable, nt_dtype table_dtype, int32_t accumulate, void* workspace,
+                                uint64_t workspace_bytes, void* stream);
+nt_status nt_embedding_backward_workspace(int64_t rows, int64_t vocab, int32_t C, uint64_t* bytes);
+
 /* Thread-local description of the last error on this thread. */
 const char* nt_last_error(void);
 

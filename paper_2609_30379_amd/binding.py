@@ -70,6 +70,19 @@ class LinearArgs(C.Structure):
                 ("gate", C.c_void_p), ("ld_gate", C.c_int64)]
 
 
+class WindowArgs(C.Structure):
+    _fields_ = [("q_layout", C.c_void_p), ("kv_layout", C.c_void_p),
+                ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("left", C.c_int32), ("right", C.c_int32), ("sinks", C.c_int32),
+                ("scale", C.c_float), ("dtype", C.c_int),
+                ("q", C.c_void_p), ("ld_q", C.c_int64), ("k", C.c_void_p), ("ld_k", C.c_int64),
+                ("v", C.c_void_p), ("ld_v", C.c_int64), ("o", C.c_void_p), ("ld_o", C.c_int64),
+                ("lse", C.c_void_p), ("ld_lse", C.c_int64), ("kv_lengths", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+                ("dout", C.c_void_p), ("ld_dout", C.c_int64), ("dq", C.c_void_p), ("ld_dq", C.c_int64),
+                ("dk", C.c_void_p), ("ld_dk", C.c_int64), ("dv", C.c_void_p), ("ld_dv", C.c_int64)]
+
+
 _lib = None
 
 
@@ -114,6 +127,13 @@ def load(path: str = LIB_PATH):
         "nt_pair_row_attention_backward": [vp, i32, i32, i32, vp, vp, vp, i64, vp, i64, i64, vp, i64, f32,
                                            vp, vp, vp, i64, vp, i64, i64, C.c_int, vp, u64, vp],
         "nt_pair_row_attention_backward_workspace": [vp, i32, i32, i32, C.c_int, C.POINTER(u64)],
+        "nt_window_attention": [C.POINTER(WindowArgs), vp],
+        "nt_window_attention_workspace": [C.POINTER(WindowArgs), C.POINTER(u64)],
+        "nt_window_attention_backward": [C.POINTER(WindowArgs), vp],
+        "nt_window_attention_backward_workspace": [C.POINTER(WindowArgs), C.POINTER(u64)],
+        "nt_embedding": [vp, i64, i64, C.c_int, vp, i32, i64, i32, f32, vp, i64, C.c_int, vp],
+        "nt_embedding_backward": [vp, i32, i64, i64, i32, vp, i64, C.c_int, f32, vp, i64, C.c_int, i32, vp, u64, vp],
+        "nt_embedding_backward_workspace": [i64, i64, i32, C.POINTER(u64)],
         "nt_last_error": [],
         "nt_version": [],
     }
@@ -171,7 +191,7 @@ def _mat(t, name):
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     shape, stride = t.shape, t.stride()
-    if len(shape) != 2 or (shape[1] > 1 and stride[1] != 1):
+    if len(shape) != 2 or (shape[0] > 0 and shape[1] > 1 and stride[1] != 1):
         raise ValueError(f"{name} must be 2-D with contiguous rows")
     return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1]
 
@@ -625,6 +645,166 @@ def nt_pair_row_attention_backward(layout: NestedLayout, axis: int, heads: int, 
                                                  pb, ldb, ldbh, pg, ldg, scale, pdq, pdk, pdv, ldd,
                                                  pdb, lddb, lddbh, _dtype(q), pw, nw, _stream()))
     return dq, dk, dv, dbias
+
+
+# ---------------------------------------------------------------- tokens
+def _same_device(*named):
+    """Raises unless every tensor given is on the current device."""
+    dev = _t().cuda.current_device()
+    for name, t in named:
+        if t is not None and (not t.is_cuda or t.device.index != dev):
+            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{dev}")
+
+
+def _rows(t, name, rows, cols):
+    """(device pointer, row stride) of a [rows, cols] operand."""
+    p, ld = _mat(t, name)
+    if t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{name} must be [{rows}, {cols}], got {list(t.shape)}")
+    return p, ld
+
+
+def _window_args(q_layout, heads, head_dim, kv_layout, kv_heads, left, right, sinks, scale, dtype) -> WindowArgs:
+    a = WindowArgs()
+    a.q_layout = q_layout.handle
+    if kv_layout is not None:
+        a.kv_layout = kv_layout.handle
+    a.heads, a.head_dim = int(heads), int(head_dim)
+    a.kv_heads = a.heads if kv_heads is None else int(kv_heads)
+    a.left, a.right, a.sinks = int(left), int(right), int(sinks)
+    a.scale = 1.0 / float(np.sqrt(head_dim)) if scale is None else float(scale)
+    a.dtype = dtype
+    return a
+
+
+def window_attention_workspace_bytes(q_layout: NestedLayout, heads: int, head_dim: int,
+                                     kv_layout: NestedLayout | None = None, kv_heads: int | None = None,
+                                     left: int = -1, right: int = 0, sinks: int = 0, dtype: str = "bf16") -> int:
+    a = _window_args(q_layout, heads, head_dim, kv_layout, kv_heads, left, right, sinks, 1.0,
+                     NT_BF16 if dtype == "bf16" else NT_F32)
+    n = C.c_uint64()
+    _check(load().nt_window_attention_workspace(C.byref(a), C.byref(n)))
+    return int(n.value)
+
+
+def window_attention_backward_workspace_bytes(q_layout: NestedLayout, heads: int, head_dim: int,
+                                              kv_layout: NestedLayout | None = None, kv_heads: int | None = None,
+                                              left: int = -1, right: int = 0, sinks: int = 0,
+                                              dtype: str = "bf16") -> int:
+    a = _window_args(q_layout, heads, head_dim, kv_layout, kv_heads, left, right, sinks, 1.0,
+                     NT_BF16 if dtype == "bf16" else NT_F32)
+    n = C.c_uint64()
+    _check(load().nt_window_attention_backward_workspace(C.byref(a), C.byref(n)))
+    return int(n.value)
+
+
+def _window_operands(a, q_layout, kv_layout, q, k, v, o, lse):
+    nq, nk = q_layout.sum_n, (q_layout if kv_layout is None else kv_layout).sum_n
+    cq, ck = a.heads * a.head_dim, a.kv_heads * a.head_dim
+    if not (q.dtype == k.dtype == v.dtype == o.dtype):
+        raise ValueError("q, k, v and o must share one dtype")
+    a.q, a.ld_q = _rows(q, "q", nq, cq)
+    a.k, a.ld_k = _rows(k, "k", nk, ck)
+    a.v, a.ld_v = _rows(v, "v", nk, ck)
+    a.o, a.ld_o = _rows(o, "o", nq, cq)
+    if lse is not None:
+        if lse.dtype != _t().float32:
+            raise ValueError("lse must be float32")
+        a.lse, a.ld_lse = _rows(lse, "lse", a.heads, nq)
+        a.ld_lse = max(a.ld_lse, nq)
+    return nq, nk, cq, ck
+
+
+def nt_window_attention(q_layout: NestedLayout, heads: int, head_dim: int, q, k, v, o,
+                        kv_layout: NestedLayout | None = None, kv_heads: int | None = None, left: int = -1,
+                        right: int = 0, sinks: int = 0, scale: float | None = None, lse=None, kv_lengths=None,
+                        workspace=None):
+    """Causal (right=0) or two-sided attention of the last N_i positions of each
+    sample's M_i keys, with a window of `left` keys before and `right` after a
+    query (-1: no bound) and the first `sinks` keys always visible.
+    q, o: [sum N, heads*head_dim]; k, v: [sum M, kv_heads*head_dim]; lse: fp32
+    [heads, sum N] (needed by the backward) or None; kv_lengths: device int32
+    [batch], the keys in use of each sample's slots, or None."""
+    a = _window_args(q_layout, heads, head_dim, kv_layout, kv_heads, left, right, sinks, scale, _dtype(q))
+    _same_device(("q", q), ("k", k), ("v", v), ("o", o), ("lse", lse), ("kv_lengths", kv_lengths),
+                 ("workspace", workspace))
+    _window_operands(a, q_layout, kv_layout, q, k, v, o, lse)
+    if kv_lengths is not None:
+        if kv_lengths.dtype != _t().int32 or kv_lengths.dim() != 1 or kv_lengths.shape[0] != q_layout.batch \
+                or not kv_lengths.is_contiguous():
+            raise ValueError("kv_lengths must be contiguous int32 [batch]")
+        a.kv_lengths = kv_lengths.data_ptr()
+    if workspace is None:
+        n = C.c_uint64()
+        _check(load().nt_window_attention_workspace(C.byref(a), C.byref(n)))
+        workspace = workspace_tensor(int(n.value))
+    a.workspace, a.workspace_bytes = _ws(workspace)
+    _check(load().nt_window_attention(C.byref(a), _stream()))
+    return o
+
+
+def nt_window_attention_backward(q_layout: NestedLayout, heads: int, head_dim: int, q, k, v, o, lse, dout, dq, dk, dv,
+                                 kv_layout: NestedLayout | None = None, kv_heads: int | None = None, left: int = -1,
+                                 right: int = 0, sinks: int = 0, scale: float | None = None, workspace=None):
+    """Gradients of nt_window_attention from its operands, its output o and lse,
+    and the output's gradient; dq, dk, dv are overwritten."""
+    a = _window_args(q_layout, heads, head_dim, kv_layout, kv_heads, left, right, sinks, scale, _dtype(q))
+    _same_device(("q", q), ("k", k), ("v", v), ("o", o), ("lse", lse), ("dout", dout), ("dq", dq), ("dk", dk),
+                 ("dv", dv), ("workspace", workspace))
+    nq, nk, cq, ck = _window_operands(a, q_layout, kv_layout, q, k, v, o, lse)
+    if any(t.dtype != q.dtype for t in (dout, dq, dk, dv)):
+        raise ValueError("dout, dq, dk and dv must have the dtype of q")
+    a.dout, a.ld_dout = _rows(dout, "dout", nq, cq)
+    a.dq, a.ld_dq = _rows(dq, "dq", nq, cq)
+    a.dk, a.ld_dk = _rows(dk, "dk", nk, ck)
+    a.dv, a.ld_dv = _rows(dv, "dv", nk, ck)
+    if workspace is None:
+        n = C.c_uint64()
+        _check(load().nt_window_attention_backward_workspace(C.byref(a), C.byref(n)))
+        workspace = workspace_tensor(int(n.value))
+    a.workspace, a.workspace_bytes = _ws(workspace)
+    _check(load().nt_window_attention_backward(C.byref(a), _stream()))
+    return dq, dk, dv
+
+
+def _ids(ids):
+    torch = _t()
+    if ids.dim() != 1 or not ids.is_contiguous() or ids.dtype not in (torch.int32, torch.int64):
+        raise ValueError("ids must be contiguous 1-D int32 or int64")
+    return ids.data_ptr(), int(ids.dtype == torch.int64), ids.shape[0]
+
+
+def nt_embedding(table, ids, y, scale: float = 1.0):
+    """y[r] = scale * table[ids[r]]; an id outside the table gives a row of zeros."""
+    _same_device(("table", table), ("ids", ids), ("y", y))
+    pi, wide, rows = _ids(ids)
+    vocab, c = table.shape
+    pt, ldt = _mat(table, "table")
+    py, ldy = _rows(y, "y", rows, c)
+    _check(load().nt_embedding(pt, vocab, ldt, _dtype(table), pi, wide, rows, c, float(scale), py, ldy, _dtype(y),
+                               _stream()))
+    return y
+
+
+def embedding_backward_workspace_bytes(rows: int, vocab: int, c: int) -> int:
+    n = C.c_uint64()
+    _check(load().nt_embedding_backward_workspace(int(rows), int(vocab), int(c), C.byref(n)))
+    return int(n.value)
+
+
+def nt_embedding_backward(ids, dy, dtable, scale: float = 1.0, accumulate: bool = False, workspace=None):
+    """dtable[v] (+)= scale * sum of dy over the rows with id v (fp32 or bf16 dtable)."""
+    _same_device(("ids", ids), ("dy", dy), ("dtable", dtable), ("workspace", workspace))
+    pi, wide, rows = _ids(ids)
+    vocab, c = dtable.shape
+    py, ldy = _rows(dy, "dy", rows, c)
+    pt, ldt = _mat(dtable, "dtable")
+    if workspace is None:
+        workspace = workspace_tensor(embedding_backward_workspace_bytes(rows, vocab, c))
+    pw, nw = _ws(workspace)
+    _check(load().nt_embedding_backward(pi, wide, rows, vocab, c, py, ldy, _dtype(dy), float(scale), pt, ldt,
+                                        _dtype(dtable), int(bool(accumulate)), pw, nw, _stream()))
+    return dtable
 
 
 def version() -> str:

@@ -770,4 +770,191 @@ nt_status nt_triangle_mul_workspace(const nt_layout* L, int32_t C, nt_tri_operan
   return NT_OK;
 }
 
+namespace {
+int32_t longest(const nt_layout* L) {
+  int32_t n = 0;
+  for (int32_t x : L->lengths) n = x > n ? x : n;
+  return n;
+}
+
+// Sizes and layouts of a window attention call, without its pointers.  On NT_OK
+// *out holds the call with kv_layout filled in and left, right and sinks brought
+// within the samples' lengths (a bound that no sample reaches becomes -1).
+nt_status window_sizes(const nt_window_args* a, nt_window_args* out) {
+  if (!a) return nt::fail(NT_ERR_INVALID_ARG, "args is NULL");
+  if (!a->q_layout) return nt::fail(NT_ERR_INVALID_ARG, "q_layout is NULL");
+  *out = *a;
+  if (!out->kv_layout) out->kv_layout = a->q_layout;
+  const nt_layout *Lq = out->q_layout, *Lk = out->kv_layout;
+  if (Lq->batch != Lk->batch)
+    return nt::fail(NT_ERR_LAYOUT_MISMATCH, "query and key layouts hold different batch sizes (" +
+                                                std::to_string(Lq->batch) + " vs " + std::to_string(Lk->batch) + ")");
+  if (!valid_dtype(a->dtype)) return nt::fail(NT_ERR_INVALID_ARG, "bad dtype");
+  if (a->heads <= 0 || a->kv_heads <= 0 || a->heads % a->kv_heads)
+    return nt::fail(NT_ERR_INVALID_ARG, "heads must be a positive multiple of kv_heads");
+  if (a->head_dim <= 0) return nt::fail(NT_ERR_INVALID_ARG, "head_dim must be > 0");
+  if (a->head_dim % 8 || a->head_dim > 128)
+    return nt::fail(NT_ERR_UNSUPPORTED, "window attention supports head_dim in multiples of 8 up to 128");
+  if (a->left < -1 || a->right < -1 || a->sinks < 0)
+    return nt::fail(NT_ERR_INVALID_ARG, "left and right must be >= -1 and sinks >= 0");
+  const int32_t n = longest(Lq), m = longest(Lk);
+  if (n >= 1 << 30 || m >= 1 << 30) return nt::fail(NT_ERR_OVERFLOW, "a sample has 2^30 tokens or more");
+  // p = M - N + t is at least -N and below M
+  if (out->left >= m) out->left = -1;
+  if (out->right >= n) out->right = -1;
+  if (out->sinks > m) out->sinks = m;
+  if (((Lq->sum_n * (a->heads / a->kv_heads) >> 5) + Lq->batch) * a->kv_heads > INT32_MAX ||
+      ((Lk->sum_n >> 5) + Lk->batch) * a->kv_heads > INT32_MAX)
+    return nt::fail(NT_ERR_OVERFLOW, "heads times tokens beyond the launch limit");
+  return NT_OK;
+}
+
+nt_status matrix_operand(const void* p, int64_t ld, int64_t width, int64_t rows, int ve, const char* name) {
+  if (rows == 0) return NT_OK;
+  if (!p) return nt::fail(NT_ERR_INVALID_ARG, std::string(name) + " is NULL");
+  if (!aligned16(p)) return nt::fail(NT_ERR_INVALID_ARG, std::string(name) + " must be 16-byte aligned");
+  if (ld < width || ld % ve)
+    return nt::fail(NT_ERR_INVALID_ARG, std::string(name) + "'s row stride must hold its heads and be a multiple of " +
+                                            std::to_string(ve));
+  return NT_OK;
+}
+
+nt_status on_current_device(const nt_layout* L) {
+  if (nt_status st = need_device(L)) return st;
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess) return nt::fail(NT_ERR_HIP, "hipGetDevice failed");
+  if (dev != L->device)
+    return nt::fail(NT_ERR_INVALID_ARG, "the layout is on device " + std::to_string(L->device) +
+                                            ", the current device is " + std::to_string(dev));
+  return NT_OK;
+}
+
+nt_status window_operands(const nt_window_args& a) {
+  const int ve = vec_elems(a.dtype);
+  const int64_t cq = (int64_t)a.heads * a.head_dim, ck = (int64_t)a.kv_heads * a.head_dim;
+  const int64_t nq = a.q_layout->sum_n, nk = a.kv_layout->sum_n;
+  if (!(a.scale - a.scale == 0.f)) return nt::fail(NT_ERR_INVALID_ARG, "scale must be finite");
+  if (nt_status st = matrix_operand(a.q, a.ld_q, cq, nq, ve, "q")) return st;
+  if (nt_status st = matrix_operand(a.k, a.ld_k, ck, nk, ve, "k")) return st;
+  if (nt_status st = matrix_operand(a.v, a.ld_v, ck, nk, ve, "v")) return st;
+  if (nt_status st = matrix_operand(a.o, a.ld_o, cq, nq, ve, "o")) return st;
+  if (a.lse && ((reinterpret_cast<uintptr_t>(a.lse) & 3u) || a.ld_lse < nq))
+    return nt::fail(NT_ERR_INVALID_ARG, "lse must be 4-byte aligned with ld_lse >= the query rows");
+  if (nt_status st = on_current_device(a.q_layout)) return st;
+  return on_current_device(a.kv_layout);
+}
+
+nt_status embedding_sizes(int64_t rows, int64_t vocab, int32_t C) {
+  if (rows < 0 || vocab < 0) return nt::fail(NT_ERR_INVALID_ARG, "rows and vocab must be >= 0");
+  if (rows > INT32_MAX || vocab >= INT32_MAX) return nt::fail(NT_ERR_OVERFLOW, "rows or vocab exceed int32");
+  if (C <= 0 || C % 8) return nt::fail(NT_ERR_INVALID_ARG, "C must be a positive multiple of 8");
+  return NT_OK;
+}
+
+nt_status embedding_ids(const void* ids, int32_t wide, int64_t rows) {
+  if (wide != 0 && wide != 1) return nt::fail(NT_ERR_INVALID_ARG, "ids_are_64 must be 0 or 1");
+  if (rows > 0 && (!ids || (reinterpret_cast<uintptr_t>(ids) & (wide ? 7u : 3u))))
+    return nt::fail(NT_ERR_INVALID_ARG, "ids must be non-NULL and element-aligned");
+  return NT_OK;
+}
+}  // namespace
+
+nt_status nt_window_attention_workspace(const nt_window_args* args, uint64_t* bytes) {
+  g_last_error.clear();
+  if (!bytes) return nt::fail(NT_ERR_INVALID_ARG, "bytes is NULL");
+  nt_window_args a;
+  if (nt_status st = window_sizes(args, &a)) return st;
+  *bytes = (uint64_t)nt::window_workspace_bytes(a);
+  return NT_OK;
+}
+
+nt_status nt_window_attention(const nt_window_args* args, void* stream) {
+  g_last_error.clear();
+  nt_window_args a;
+  if (nt_status st = window_sizes(args, &a)) return st;
+  if (nt_status st = window_operands(a)) return st;
+  if (a.kv_lengths && (reinterpret_cast<uintptr_t>(a.kv_lengths) & 3u))
+    return nt::fail(NT_ERR_INVALID_ARG, "kv_lengths must be 4-byte aligned");
+  if (a.q_layout->sum_n == 0) return NT_OK;
+  if (nt_status st = need_workspace(nt::window_workspace_bytes(a), a.workspace, a.workspace_bytes,
+                                    "nt_window_attention_workspace"))
+    return st;
+  return check_hip(nt::launch_window(a, static_cast<hipStream_t>(stream)), "nt_window_attention launch");
+}
+
+nt_status nt_window_attention_backward_workspace(const nt_window_args* args, uint64_t* bytes) {
+  g_last_error.clear();
+  if (!bytes) return nt::fail(NT_ERR_INVALID_ARG, "bytes is NULL");
+  nt_window_args a;
+  if (nt_status st = window_sizes(args, &a)) return st;
+  *bytes = (uint64_t)nt::window_backward_workspace_bytes(a);
+  return NT_OK;
+}
+
+nt_status nt_window_attention_backward(const nt_window_args* args, void* stream) {
+  g_last_error.clear();
+  nt_window_args a;
+  if (nt_status st = window_sizes(args, &a)) return st;
+  if (a.kv_lengths) return nt::fail(NT_ERR_INVALID_ARG, "the backward takes no kv_lengths");
+  if (nt_status st = window_operands(a)) return st;
+  const int ve = vec_elems(a.dtype);
+  const int64_t cq = (int64_t)a.heads * a.head_dim, ck = (int64_t)a.kv_heads * a.head_dim;
+  const int64_t nq = a.q_layout->sum_n, nk = a.kv_layout->sum_n;
+  if (nq > 0 && !a.lse) return nt::fail(NT_ERR_INVALID_ARG, "the backward needs the forward's lse");
+  if (nt_status st = matrix_operand(a.dout, a.ld_dout, cq, nq, ve, "dout")) return st;
+  if (nt_status st = matrix_operand(a.dq, a.ld_dq, cq, nq, ve, "dq")) return st;
+  if (nt_status st = matrix_operand(a.dk, a.ld_dk, ck, nk, ve, "dk")) return st;
+  if (nt_status st = matrix_operand(a.dv, a.ld_dv, ck, nk, ve, "dv")) return st;
+  if (nq == 0 && nk == 0) return NT_OK;
+  if (nt_status st = need_workspace(nt::window_backward_workspace_bytes(a), a.workspace, a.workspace_bytes,
+                                    "nt_window_attention_backward_workspace"))
+    return st;
+  return check_hip(nt::launch_window_backward(a, static_cast<hipStream_t>(stream)),
+                   "nt_window_attention_backward launch");
+}
+
+nt_status nt_embedding(const void* table, int64_t vocab, int64_t ld_table, nt_dtype table_dtype, const void* ids,
+                       int32_t ids_are_64, int64_t rows, int32_t C, float scale, void* y, int64_t ld_y,
+                       nt_dtype y_dtype, void* stream) {
+  g_last_error.clear();
+  if (nt_status st = embedding_sizes(rows, vocab, C)) return st;
+  if (!valid_dtype(table_dtype) || !valid_dtype(y_dtype)) return nt::fail(NT_ERR_INVALID_ARG, "bad dtype");
+  if (nt_status st = embedding_ids(ids, ids_are_64, rows)) return st;
+  if (nt_status st = matrix_operand(table, ld_table, C, vocab, vec_elems(table_dtype), "table")) return st;
+  if (nt_status st = matrix_operand(y, ld_y, C, rows, vec_elems(y_dtype), "y")) return st;
+  if (rows == 0) return NT_OK;
+  return check_hip(nt::launch_embedding(table, vocab, ld_table, table_dtype, ids, ids_are_64, rows, C, scale, y, ld_y,
+                                        y_dtype, static_cast<hipStream_t>(stream)),
+                   "nt_embedding launch");
+}
+
+nt_status nt_embedding_backward_workspace(int64_t rows, int64_t vocab, int32_t C, uint64_t* bytes) {
+  g_last_error.clear();
+  if (!bytes) return nt::fail(NT_ERR_INVALID_ARG, "bytes is NULL");
+  if (nt_status st = embedding_sizes(rows, vocab, C)) return st;
+  *bytes = (uint64_t)nt::embedding_backward_workspace_bytes(rows, vocab, C);
+  return NT_OK;
+}
+
+nt_status nt_embedding_backward(const void* ids, int32_t ids_are_64, int64_t rows, int64_t vocab, int32_t C,
+                                const void* dy, int64_t ld_dy, nt_dtype dtype, float scale, void* dtable,
+                                int64_t ld_dtable, nt_dtype table_dtype, int32_t accumulate, void* workspace,
+                                uint64_t workspace_bytes, void* stream) {
+  g_last_error.clear();
+  if (nt_status st = embedding_sizes(rows, vocab, C)) return st;
+  if (!valid_dtype(dtype) || !valid_dtype(table_dtype)) return nt::fail(NT_ERR_INVALID_ARG, "bad dtype");
+  if (accumulate != 0 && accumulate != 1) return nt::fail(NT_ERR_INVALID_ARG, "accumulate must be 0 or 1");
+  if (nt_status st = embedding_ids(ids, ids_are_64, rows)) return st;
+  if (nt_status st = matrix_operand(dy, ld_dy, C, rows, vec_elems(dtype), "dy")) return st;
+  if (nt_status st = matrix_operand(dtable, ld_dtable, C, vocab, vec_elems(table_dtype), "dtable")) return st;
+  if (vocab == 0 || (rows == 0 && accumulate)) return NT_OK;
+  if (nt_status st = need_workspace(nt::embedding_backward_workspace_bytes(rows, vocab, C), workspace, workspace_bytes,
+                                    "nt_embedding_backward_workspace"))
+    return st;
+  return check_hip(nt::launch_embedding_backward(ids, ids_are_64, rows, vocab, C, dy, ld_dy, dtype, scale, dtable,
+                                                 ld_dtable, table_dtype, accumulate, workspace,
+                                                 static_cast<hipStream_t>(stream)),
+                   "nt_embedding_backward launch");
+}
+
 }  // extern "C"

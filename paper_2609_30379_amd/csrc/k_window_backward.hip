@@ -1,0 +1,344 @@
+// Backward of the sliding-window attention (k_window.hip): the weights are
+// recomputed from the forward's lse,
+//   P = exp(s - lse),  D = sum_c dO O,  dS = P (dO V^T - D)
+//   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO.
+// Two passes without atomics: one over the keys of 128 query rows (dQ, and D for
+// the second pass), one over the query rows of 128 keys (dK, dV; the rows of all
+// query heads that share the keys are one sequence, so a shared head's gradient
+// is one accumulator).  Both hold their 32 rows or keys per wave as columns of
+// the products, so P and dS go from accumulators into the next operand in
+// registers.
+#include "window_device.h"
+
+namespace nt {
+namespace {
+using namespace win;
+
+struct WindowBwdParams {
+  const int32_t *cu_q, *cu_k;
+  int batch, heads, kv_heads, group, d, left, right, sinks;
+  float scale, c;                // c = scale * log2(e)
+  const void *q, *k, *v, *o, *dout;
+  void *dq, *dk, *dv;
+  int64_t ld_q, ld_k, ld_v, ld_o, ld_dout, ld_dq, ld_dk, ld_dv, ld_lse;
+  const float* lse;
+  float* delta;                  // [heads][sum N] workspace
+  int64_t sum_q;
+  int64_t items;
+};
+
+constexpr int kBlockShift = 7;
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(256)
+window_dq_kernel(WindowBwdParams p) {
+  typedef typename Frag<T>::type frag;
+  constexpr int KT = sizeof(T) == 2 ? 64 : 32, KB = KT / 32, NS = DP / 16, ND = DP / 32;
+  __shared__ __attribute__((aligned(16))) T Ks[KT * Tile<T, DP>::kLd];
+  __shared__ __attribute__((aligned(16))) T Vs[KT * Tile<T, DP>::kLd];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h32 = lane >> 5;
+  const int64_t item = block_id();
+  if (item >= p.items) return;
+  const int hk = (int)(item % p.kv_heads);
+  const int64_t b = item / p.kv_heads;
+  const int i = find_sample(p.cu_q, p.batch, p.group, kBlockShift, b, lane);
+  const int q0 = p.cu_q[i], n = p.cu_q[i + 1] - q0, k0 = p.cu_k[i], m = p.cu_k[i + 1] - k0;
+  const int64_t rows = (int64_t)n * p.group, r0 = (b - block_start(p.cu_q, i, p.group, kBlockShift)) << kBlockShift;
+  if (r0 >= rows) return;
+  const int t0 = (int)(r0 / p.group), g0 = (int)(r0 - (int64_t)t0 * p.group);
+  const int last = (int)min((int64_t)127, rows - 1 - r0), off = m - n;
+  const int x = min(wave * 32 + (lane & 31), last), tg = (g0 + x) / p.group;
+  const int t = t0 + tg, g = g0 + x - tg * p.group, pos = off + t, head = hk * p.group + g;
+  const int lo = p.left >= 0 ? pos - p.left : 0, hi = p.right >= 0 ? min(pos + p.right, m - 1) : m - 1;
+  const bool live = wave * 32 <= last, mine = wave * 32 + (lane & 31) <= last;
+
+  frag Q[NS], G[NS];
+  float delta = 0.f;
+  {
+    const T* src = (const T*)p.q + (int64_t)(q0 + t) * p.ld_q + (int64_t)head * p.d;
+    const T* dsrc = (const T*)p.dout + (int64_t)(q0 + t) * p.ld_dout + (int64_t)head * p.d;
+    const T* osrc = (const T*)p.o + (int64_t)(q0 + t) * p.ld_o + (int64_t)head * p.d;
+#pragma unroll
+    for (int ks = 0; ks < NS; ++ks) {
+      const int e = 16 * ks + 8 * h32;
+      frag z = {}, o = {};
+      Q[ks] = e < p.d ? *reinterpret_cast<const frag*>(src + e) : z;
+      G[ks] = e < p.d ? *reinterpret_cast<const frag*>(dsrc + e) : z;
+      if (e < p.d) o = *reinterpret_cast<const frag*>(osrc + e);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) delta = fmaf((float)o[u], (float)G[ks][u], delta);
+    }
+    delta = pair_sum(delta);
+  }
+  const float lse2 = p.lse[(int64_t)head * p.ld_lse + q0 + t] * kLog2e;
+  if (mine && h32 == 0) p.delta[(int64_t)head * p.sum_q + q0 + t] = delta;
+  uint32_t tr[2];
+  Tile<T, DP>::across_addr(lane, tr);
+
+  f32x16 dQ[ND];
+#pragma unroll
+  for (int dt = 0; dt < ND; ++dt) dQ[dt] = f32x16{};
+
+  const KeyTiles kt(off + t0, off + t0 + (g0 + last) / p.group, m, p.left, p.right, p.sinks, KT);
+  const T* kbase = (const T*)p.k + (int64_t)hk * p.d;
+  const T* vbase = (const T*)p.v + (int64_t)hk * p.d;
+  Stage<T, DP, KT, 256> sk, sv;
+  auto load = [&](int tile) {
+    const int j0 = kt.first(tile, KT), cnt = kt.end(tile) - j0;
+    sk.load(tid, cnt, p.d, [&](int r) { return kbase + (int64_t)(k0 + j0 + r) * p.ld_k; });
+    sv.load(tid, cnt, p.d, [&](int r) { return vbase + (int64_t)(k0 + j0 + r) * p.ld_v; });
+  };
+  if (kt.n > 0) load(0);
+  for (int tile = 0; tile < kt.n; ++tile) {
+    __syncthreads();
+    sk.store(tid, Ks);
+    sv.store(tid, Vs);
+    __syncthreads();
+    const int j0 = kt.first(tile, KT), jend = kt.end(tile);
+    if (tile + 1 < kt.n) load(tile + 1);
+    if (!live) continue;
+    const int je = min(j0 + KT, jend);
+    if (!__any(j0 <= hi && (je > lo || j0 < p.sinks))) continue;
+    const bool whole = __all(j0 + KT <= jend && j0 + KT - 1 <= hi && (j0 >= lo || j0 + KT <= p.sinks));
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      f32x16 S = f32x16{}, dP = f32x16{};
+#pragma unroll
+      for (int ks = 0; ks < NS; ++ks) {
+        S = mma32(Tile<T, DP>::along(Ks, 32 * kb, ks, lane), Q[ks], S);
+        dP = mma32(Tile<T, DP>::along(Vs, 32 * kb, ks, lane), G[ks], dP);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float ds = __builtin_amdgcn_exp2f(fmaf(S[e], p.c, -lse2)) * (dP[e] - delta);
+        if (!whole) {
+          const int j = j0 + 32 * kb + 8 * (e >> 2) + 4 * h32 + (e & 3);
+          ds = j < jend && j <= hi && (j >= lo || j < p.sinks) ? ds : 0.f;
+        }
+        S[e] = ds;
+      }
+#pragma unroll
+      for (int nn = 0; nn < 2; ++nn) {
+        frag D;
+        to_operand(S, nn, D);
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+          dQ[dt] = mma32(across<DP>(Ks, 32 * kb + 16 * nn, dt, lane, tr), D, dQ[dt]);
+      }
+    }
+  }
+  if (!mine) return;
+  T* dst = (T*)p.dq + (int64_t)(q0 + t) * p.ld_dq + (int64_t)head * p.d;
+#pragma unroll
+  for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+      const int at = 32 * dt + 2 * e + 4 * h32;
+      if (at < p.d) {
+        typedef T vec4 __attribute__((ext_vector_type(4)));
+        vec4 w;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) w[u] = (T)(dQ[dt][e + u] * p.scale);
+        *reinterpret_cast<vec4*>(dst + at) = w;
+      }
+    }
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(256)
+window_dkv_kernel(WindowBwdParams p) {
+  typedef typename Frag<T>::type frag;
+  constexpr int RT = sizeof(T) == 2 ? 64 : 32, RB = RT / 32, NS = DP / 16, ND = DP / 32;
+  __shared__ __attribute__((aligned(16))) T Qs[RT * Tile<T, DP>::kLd];
+  __shared__ __attribute__((aligned(16))) T Gs[RT * Tile<T, DP>::kLd];
+  __shared__ __attribute__((aligned(16))) float lse_s[RT];
+  __shared__ __attribute__((aligned(16))) float delta_s[RT];
+  __shared__ __attribute__((aligned(16))) int pos_s[RT];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h32 = lane >> 5;
+  const int64_t item = block_id();
+  if (item >= p.items) return;
+  const int hk = (int)(item % p.kv_heads);
+  const int64_t b = item / p.kv_heads;
+  const int i = find_sample(p.cu_k, p.batch, 1, kBlockShift, b, lane);
+  const int q0 = p.cu_q[i], n = p.cu_q[i + 1] - q0, k0 = p.cu_k[i], m = p.cu_k[i + 1] - k0;
+  const int64_t jb64 = (b - block_start(p.cu_k, i, 1, kBlockShift)) << kBlockShift;
+  if (jb64 >= m) return;
+  const int jb = (int)jb64, jl = min(jb + 127, m - 1);          // keys jb .. jl
+  const int off = m - n;
+  const int j = min(jb + wave * 32 + (lane & 31), m - 1);       // a lane past the last key takes the last one, not stored
+  const bool live = jb + wave * 32 < m, mine = jb + wave * 32 + (lane & 31) < m;
+  // positions of the rows that see key j
+  const int plo = p.right >= 0 ? j - p.right : INT32_MIN + 1;
+  const int phi = p.left >= 0 && j >= p.sinks ? j + p.left : INT32_MAX;
+
+  frag K[NS], V[NS];
+  {
+    const T* ksrc = (const T*)p.k + (int64_t)(k0 + j) * p.ld_k + (int64_t)hk * p.d;
+    const T* vsrc = (const T*)p.v + (int64_t)(k0 + j) * p.ld_v + (int64_t)hk * p.d;
+#pragma unroll
+    for (int ks = 0; ks < NS; ++ks) {
+      const int e = 16 * ks + 8 * h32;
+      frag z = {};
+      K[ks] = e < p.d ? *reinterpret_cast<const frag*>(ksrc + e) : z;
+      V[ks] = e < p.d ? *reinterpret_cast<const frag*>(vsrc + e) : z;
+    }
+  }
+  uint32_t tr[2];
+  Tile<T, DP>::across_addr(lane, tr);
+  f32x16 dK[ND], dV[ND];
+#pragma unroll
+  for (int dt = 0; dt < ND; ++dt) dK[dt] = dV[dt] = f32x16{};
+
+  // queries that see a key of the block, as rows [ra, rb)
+  const int ta = p.right >= 0 ? min(max(0, jb - p.right - off), n) : 0;
+  const int tb = p.left >= 0 && jb >= p.sinks ? min(n, max(0, jl + p.left - off + 1)) : n;
+  const int64_t ra = (int64_t)ta * p.group, rb = (int64_t)max(ta, tb) * p.group;
+  const int tiles = (int)((rb - ra + RT - 1) / RT);
+  Stage<T, DP, RT, 256> sq, sg;
+  float r_lse = 0.f, r_delta = 0.f;
+  int r_pos = 0;
+  auto load = [&](int tile) {
+    const int64_t r0 = ra + (int64_t)tile * RT;
+    const int t0 = (int)(r0 / p.group), g0 = (int)(r0 - (int64_t)t0 * p.group);
+    const int cnt = (int)min((int64_t)RT, rb - r0);
+    const int first = q0 + t0, h0 = hk * p.group;
+    auto at = [&](const void* base, int64_t ld, int r) {
+      const int tg = (g0 + r) / p.group;
+      return (const T*)base + (int64_t)(first + tg) * ld + (int64_t)(h0 + g0 + r - tg * p.group) * p.d;
+    };
+    sq.load(tid, cnt, p.d, [&](int r) { return at(p.q, p.ld_q, r); });
+    sg.load(tid, cnt, p.d, [&](int r) { return at(p.dout, p.ld_dout, r); });
+    if (tid < RT) {
+      const int r = min(tid, cnt - 1), tg = (g0 + r) / p.group, head = h0 + g0 + r - tg * p.group;
+      r_lse = p.lse[(int64_t)head * p.ld_lse + first + tg] * kLog2e;
+      r_delta = p.delta[(int64_t)head * p.sum_q + first + tg];
+      r_pos = tid < cnt ? off + t0 + tg : INT32_MIN;            // no key sees a row past the end
+    }
+  };
+  if (tiles > 0) load(0);
+  for (int tile = 0; tile < tiles; ++tile) {
+    __syncthreads();
+    sq.store(tid, Qs);
+    sg.store(tid, Gs);
+    if (tid < RT) {
+      lse_s[tid] = r_lse;
+      delta_s[tid] = r_delta;
+      pos_s[tid] = r_pos;
+    }
+    __syncthreads();
+    const int64_t r0 = ra + (int64_t)tile * RT;
+    if (tile + 1 < tiles) load(tile + 1);
+    if (!live) continue;
+    const int pa = off + (int)(r0 / p.group), pe = off + (int)((min(r0 + RT, rb) - 1) / p.group);
+    if (!__any(pe >= plo && pa <= phi)) continue;
+    const bool whole = __all(r0 + RT <= rb && pa >= plo && pe <= phi);
+#pragma unroll
+    for (int rbk = 0; rbk < RB; ++rbk) {
+      f32x16 S = f32x16{}, dP = f32x16{};
+#pragma unroll
+      for (int ks = 0; ks < NS; ++ks) {
+        S = mma32(Tile<T, DP>::along(Qs, 32 * rbk, ks, lane), K[ks], S);
+        dP = mma32(Tile<T, DP>::along(Gs, 32 * rbk, ks, lane), V[ks], dP);
+      }
+#pragma unroll
+      for (int e4 = 0; e4 < 4; ++e4) {
+        const int r = 32 * rbk + 8 * e4 + 4 * h32;
+        const f32x4 ls = *reinterpret_cast<const f32x4*>(lse_s + r), de = *reinterpret_cast<const f32x4*>(delta_s + r);
+        const int4 ps = *reinterpret_cast<const int4*>(pos_s + r);
+        const int pr[4] = {ps.x, ps.y, ps.z, ps.w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int e = 4 * e4 + u;
+          float w = __builtin_amdgcn_exp2f(fmaf(S[e], p.c, -ls[u]));
+          float ds = w * (dP[e] - de[u]);
+          if (!whole) {
+            const bool seen = pr[u] >= plo && pr[u] <= phi;
+            w = seen ? w : 0.f;
+            ds = seen ? ds : 0.f;
+          }
+          S[e] = w;
+          dP[e] = ds;
+        }
+      }
+#pragma unroll
+      for (int nn = 0; nn < 2; ++nn) {
+        frag W, D;
+        to_operand(S, nn, W);
+        to_operand(dP, nn, D);
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) {
+          dV[dt] = mma32(across<DP>(Gs, 32 * rbk + 16 * nn, dt, lane, tr), W, dV[dt]);
+          dK[dt] = mma32(across<DP>(Qs, 32 * rbk + 16 * nn, dt, lane, tr), D, dK[dt]);
+        }
+      }
+    }
+  }
+  if (!mine) return;
+  T* kd = (T*)p.dk + (int64_t)(k0 + j) * p.ld_dk + (int64_t)hk * p.d;
+  T* vd = (T*)p.dv + (int64_t)(k0 + j) * p.ld_dv + (int64_t)hk * p.d;
+#pragma unroll
+  for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+      const int at = 32 * dt + 2 * e + 4 * h32;
+      if (at < p.d) {
+        typedef T vec4 __attribute__((ext_vector_type(4)));
+        vec4 a, w;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          a[u] = (T)(dK[dt][e + u] * p.scale);
+          w[u] = (T)dV[dt][e + u];
+        }
+        *reinterpret_cast<vec4*>(kd + at) = a;
+        *reinterpret_cast<vec4*>(vd + at) = w;
+      }
+    }
+}
+
+template <typename T, int DP>
+hipError_t launch_backward(WindowBwdParams p, int64_t q_items, int64_t k_items, hipStream_t s) {
+  p.items = q_items;
+  if (q_items > 0) window_dq_kernel<T, DP><<<folded_grid(q_items), 256, 0, s>>>(p);
+  if (hipError_t e = hipGetLastError()) return e;
+  p.items = k_items;
+  if (k_items > 0) window_dkv_kernel<T, DP><<<folded_grid(k_items), 256, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t window_backward_workspace_bytes(const nt_window_args& a) {
+  return ((size_t)a.heads * a.q_layout->sum_n * sizeof(float) + 15) / 16 * 16;
+}
+
+hipError_t launch_window_backward(const nt_window_args& a, hipStream_t s) {
+  const nt_layout &Lq = *a.q_layout, &Lk = a.kv_layout ? *a.kv_layout : Lq;
+  WindowBwdParams p{};
+  p.cu_q = Lq.d_cu_seqlens;
+  p.cu_k = Lk.d_cu_seqlens;
+  p.batch = Lq.batch;
+  p.heads = a.heads;
+  p.kv_heads = a.kv_heads;
+  p.group = a.heads / a.kv_heads;
+  p.d = a.head_dim;
+  p.left = a.left;
+  p.right = a.right;
+  p.sinks = a.sinks;
+  p.scale = a.scale;
+  p.c = a.scale * win::kLog2e;
+  p.q = a.q; p.k = a.k; p.v = a.v; p.o = a.o; p.dout = a.dout;
+  p.dq = a.dq; p.dk = a.dk; p.dv = a.dv;
+  p.ld_q = a.ld_q; p.ld_k = a.ld_k; p.ld_v = a.ld_v; p.ld_o = a.ld_o; p.ld_dout = a.ld_dout;
+  p.ld_dq = a.ld_dq; p.ld_dk = a.ld_dk; p.ld_dv = a.ld_dv; p.ld_lse = a.ld_lse;
+  p.lse = a.lse;
+  p.delta = (float*)a.workspace;
+  p.sum_q = Lq.sum_n;
+  const int64_t qi = Lq.sum_n ? win::block_count(Lq.sum_n, Lq.batch, p.group, kBlockShift) * p.kv_heads : 0;
+  const int64_t ki = Lk.sum_n ? win::block_count(Lk.sum_n, Lk.batch, 1, kBlockShift) * p.kv_heads : 0;
+  const bool bf = a.dtype == NT_BF16;
+  if (p.d <= 32) return bf ? launch_backward<bf16, 32>(p, qi, ki, s) : launch_backward<float, 32>(p, qi, ki, s);
+  if (p.d <= 64) return bf ? launch_backward<bf16, 64>(p, qi, ki, s) : launch_backward<float, 64>(p, qi, ki, s);
+  return bf ? launch_backward<bf16, 128>(p, qi, ki, s) : launch_backward<float, 128>(p, qi, ki, s);
+}
+
+}  // namespace nt

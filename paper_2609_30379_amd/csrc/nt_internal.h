@@ -276,6 +276,23 @@ hipError_t launch_triangle_backward(const nt_layout& L, int direction, int C, co
                                     int64_t ld_ab, const void* dt, int64_t ld_dt, void* da, void* db,
                                     int64_t ld_dab, nt_dtype dtype, void* workspace, hipStream_t s);
 
+// Window attention (k_window.hip, k_window_backward.hip).  The arguments are
+// checked and left, right and sinks brought within the samples' lengths by the
+// caller (normalised_window).
+size_t window_workspace_bytes(const nt_window_args& a);
+hipError_t launch_window(const nt_window_args& a, hipStream_t s);
+size_t window_backward_workspace_bytes(const nt_window_args& a);
+hipError_t launch_window_backward(const nt_window_args& a, hipStream_t s);
+
+// Embedding (k_embedding.hip): vocab and rows within int32, C % 8 == 0.
+size_t embedding_backward_workspace_bytes(int64_t rows, int64_t vocab, int C);
+hipError_t launch_embedding(const void* table, int64_t vocab, int64_t ld_table, nt_dtype table_dtype, const void* ids,
+                            int wide, int64_t rows, int C, float scale, void* y, int64_t ld_y, nt_dtype y_dtype,
+                            hipStream_t s);
+hipError_t launch_embedding_backward(const void* ids, int wide, int64_t rows, int64_t vocab, int C, const void* dy,
+                                     int64_t ld_dy, nt_dtype dtype, float scale, void* dtable, int64_t ld_dtable,
+                                     nt_dtype table_dtype, int accumulate, void* ws, hipStream_t s);
+
 // Host-side planner (pure C++; no HIP calls).  Fills every host array of the
 // layout from the lengths, or returns an error status.
 // cols non-NULL: rectangular pairs N_i x M_i (M_i = cols[i]).
