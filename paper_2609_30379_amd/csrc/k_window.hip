@@ -16,7 +16,7 @@ using namespace win;
 struct WindowParams {
   const int32_t *cu_q, *cu_k, *kv_lengths;
   int batch, heads, kv_heads, group, d, left, right, sinks;
-  float c;                       // scale * log2(e)
+  float c, qmul;                 // |scale| log2(e) (1 for scale 0), and what Q is multiplied by: 1, -1 or 0
   const void *q, *k, *v;
   void* o;
   int64_t ld_q, ld_k, ld_v, ld_o, ld_lse;
@@ -27,7 +27,7 @@ struct WindowParams {
 constexpr int kBlockShift = 7;                 // query rows per workgroup: 4 waves x 32
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, DP == 128 ? 2 : 3)
 window_rows_kernel(WindowParams p) {
   typedef typename Frag<T>::type frag;
   constexpr int KT = sizeof(T) == 2 ? 64 : 32, KB = KT / 32, NS = DP / 16, ND = DP / 32;
@@ -63,6 +63,11 @@ window_rows_kernel(WindowParams p) {
       frag z = {};
       Q[ks] = e < p.d ? *reinterpret_cast<const frag*>(src + e) : z;
     }
+    if (p.qmul != 1.f)
+#pragma unroll
+      for (int ks = 0; ks < NS; ++ks)
+#pragma unroll
+        for (int u = 0; u < 8; ++u) Q[ks][u] = (T)((float)Q[ks][u] * p.qmul);
   }
   uint32_t tr[2];
   Tile<T, DP>::across_addr(lane, tr);
@@ -101,36 +106,43 @@ window_rows_kernel(WindowParams p) {
 #pragma unroll
       for (int ks = 0; ks < NS; ++ks) S[kb] = mma32(Tile<T, DP>::along(Ks, 32 * kb, ks, lane), Q[ks], S[kb]);
     }
-    float top = -INFINITY;
+    if (!whole)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int j = j0 + 32 * kb + 8 * (e >> 2) + 4 * h32 + (e & 3);
+          S[kb][e] = j < jend && j <= hi && (j >= lo || j < p.sinks) ? S[kb][e] : -INFINITY;
+        }
+    float top = S[0][0];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        float s = S[kb][e] * p.c;
-        if (!whole) {
-          const int j = j0 + 32 * kb + 8 * (e >> 2) + 4 * h32 + (e & 3);
-          s = j < jend && j <= hi && (j >= lo || j < p.sinks) ? s : -INFINITY;
-        }
-        S[kb][e] = s;
-        top = fmaxf(top, s);
-      }
-    const float m_new = fmaxf(mx, pair_max(top));
-    const float sub = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = __builtin_amdgcn_exp2f(mx - sub);
-    mx = m_new;
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, S[kb][e]);
+    top *= p.c;
+    // The maximum in use only has to keep the weights within range: it moves on
+    // when a row's score passes it by 8 (weights up to 2^8), which after the
+    // first tiles is rare, and the accumulators are rescaled only then.
+    if (__any(top > mx + 8.f)) {
+      const float m_new = fmaxf(mx, pair_max(top));
+      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mx - m_new);
+      mx = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) O[dt][e] *= alpha;
+    }
+    const float sub = mx == -INFINITY ? 0.f : mx;
     float sum = 0.f;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        S[kb][e] = __builtin_amdgcn_exp2f(S[kb][e] - sub);
+        S[kb][e] = __builtin_amdgcn_exp2f(fmaf(S[kb][e], p.c, -sub));
         sum += S[kb][e];
       }
-    l = l * alpha + sum;
-#pragma unroll
-    for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) O[dt][e] *= alpha;
+    l += sum;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -176,7 +188,7 @@ hipError_t launch_rows(const WindowParams& p, hipStream_t s) {
 size_t window_workspace_bytes(const nt_window_args& a) { return 0; }
 
 hipError_t launch_window(const nt_window_args& a, hipStream_t s) {
-  const nt_layout &Lq = *a.q_layout, &Lk = a.kv_layout ? *a.kv_layout : Lq;
+  const nt_layout &Lq = *a.q_layout, &Lk = *a.kv_layout;
   WindowParams p{};
   p.cu_q = Lq.d_cu_seqlens;
   p.cu_k = Lk.d_cu_seqlens;
@@ -189,7 +201,8 @@ hipError_t launch_window(const nt_window_args& a, hipStream_t s) {
   p.left = a.left;
   p.right = a.right;
   p.sinks = a.sinks;
-  p.c = a.scale * win::kLog2e;
+  p.c = a.scale == 0.f ? 1.f : fabsf(a.scale) * win::kLog2e;
+  p.qmul = a.scale == 0.f ? 0.f : a.scale < 0.f ? -1.f : 1.f;
   p.q = a.q; p.k = a.k; p.v = a.v; p.o = a.o;
   p.ld_q = a.ld_q; p.ld_k = a.ld_k; p.ld_v = a.ld_v; p.ld_o = a.ld_o; p.ld_lse = a.ld_lse;
   p.lse = a.lse;

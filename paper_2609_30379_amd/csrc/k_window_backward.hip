@@ -8,6 +8,8 @@
 // is one accumulator).  Both hold their 32 rows or keys per wave as columns of
 // the products, so P and dS go from accumulators into the next operand in
 // registers.
+#include <algorithm>
+
 #include "window_device.h"
 
 namespace nt {
@@ -25,12 +27,20 @@ struct WindowBwdParams {
   float* delta;                  // [heads][sum N] workspace
   int64_t sum_q;
   int64_t items;
+  // gradients of the sinks from the queries past their window (window_sink_kernel)
+  int split;                     // done apart, in pieces of `piece` rows
+  int subs, pieces, piece;       // blocks of 32 sinks, most pieces of a sample, rows per piece
+  float *sink_part, *sink_sum;   // [batch][kv_heads][subs][pieces][2][32][DP], [batch][kv_heads][subs][2][32][DP]
 };
+
+// First query past the window of the keys jb .. jl; the queries before it are
+// gone through by the keys' own workgroup.
+__device__ __forceinline__ int window_end(int jl, int left, int off, int n) { return min(n, max(0, jl + left - off + 1)); }
 
 constexpr int kBlockShift = 7;
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, DP == 32 ? 3 : DP == 128 && sizeof(T) == 4 ? 1 : 2)
 window_dq_kernel(WindowBwdParams p) {
   typedef typename Frag<T>::type frag;
   constexpr int KT = sizeof(T) == 2 ? 64 : 32, KB = KT / 32, NS = DP / 16, ND = DP / 32;
@@ -145,7 +155,7 @@ window_dq_kernel(WindowBwdParams p) {
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, DP == 128 ? 1 : 2)
 window_dkv_kernel(WindowBwdParams p) {
   typedef typename Frag<T>::type frag;
   constexpr int RT = sizeof(T) == 2 ? 64 : 32, RB = RT / 32, NS = DP / 16, ND = DP / 32;
@@ -191,7 +201,7 @@ window_dkv_kernel(WindowBwdParams p) {
 
   // queries that see a key of the block, as rows [ra, rb)
   const int ta = p.right >= 0 ? min(max(0, jb - p.right - off), n) : 0;
-  const int tb = p.left >= 0 && jb >= p.sinks ? min(n, max(0, jl + p.left - off + 1)) : n;
+  const int tb = p.left >= 0 && (jb >= p.sinks || p.split) ? window_end(jl, p.left, off, n) : n;
   const int64_t ra = (int64_t)ta * p.group, rb = (int64_t)max(ta, tb) * p.group;
   const int tiles = (int)((rb - ra + RT - 1) / RT);
   Stage<T, DP, RT, 256> sq, sg;
@@ -274,6 +284,21 @@ window_dkv_kernel(WindowBwdParams p) {
     }
   }
   if (!mine) return;
+  if (p.split && j < p.sinks && max(ta, tb) < n) {         // what the queries past the window add to a sink
+    const float* sum = p.sink_sum + (((int64_t)(i * p.kv_heads + hk) * p.subs + (j >> 5)) * 64 + (j & 31)) * DP;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int at = 32 * dt + 2 * e + 4 * h32;
+        const f32x4 a = *reinterpret_cast<const f32x4*>(sum + at), w = *reinterpret_cast<const f32x4*>(sum + 32 * DP + at);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          dK[dt][e + u] += a[u];
+          dV[dt][e + u] += w[u];
+        }
+      }
+  }
   T* kd = (T*)p.dk + (int64_t)(k0 + j) * p.ld_dk + (int64_t)hk * p.d;
   T* vd = (T*)p.dv + (int64_t)(k0 + j) * p.ld_dv + (int64_t)hk * p.d;
 #pragma unroll
@@ -295,11 +320,202 @@ window_dkv_kernel(WindowBwdParams p) {
     }
 }
 
+// The sinks' gradients from the queries past their window: few keys and all the
+// later rows of the sample, which one workgroup per block of keys would walk
+// alone while the others have left.  A workgroup takes 32 sinks and a piece of
+// the rows, 32 rows of each tile of 128 per wave; every row sees every sink here,
+// so there is no mask.  The waves' sums are added in order through LDS, the
+// pieces' by sink_sum_kernel.
+template <typename T, int DP>
+__global__ void __launch_bounds__(256)
+window_sink_kernel(WindowBwdParams p) {
+  typedef typename Frag<T>::type frag;
+  constexpr int RT = 128, NS = DP / 16, ND = DP / 32;
+  union Shared {
+    struct {
+      T q[RT * Tile<T, DP>::kLd], g[RT * Tile<T, DP>::kLd];
+      float lse[RT], delta[RT];
+    } t;
+    float sum[4][32 * DP];
+  };
+  __shared__ __attribute__((aligned(16))) Shared sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h32 = lane >> 5;
+  const int64_t item = block_id();
+  if (item >= p.items) return;
+  const int hk = (int)(item % p.kv_heads), piece = (int)(item / p.kv_heads % p.pieces);
+  const int sub = (int)(item / p.kv_heads / p.pieces % p.subs), i = (int)(item / p.kv_heads / p.pieces / p.subs);
+  const int q0 = p.cu_q[i], n = p.cu_q[i + 1] - q0, k0 = p.cu_k[i], m = p.cu_k[i + 1] - k0, off = m - n;
+  const int sinks = min(p.sinks, m);
+  if (sub * 32 >= sinks) return;
+  const int jb = sub * 32 & ~127, jl = min(jb + 127, m - 1);
+  const int ta = p.right >= 0 ? min(max(0, jb - p.right - off), n) : 0;
+  const int64_t ra = (int64_t)max(ta, window_end(jl, p.left, off, n)) * p.group + (int64_t)piece * p.piece;
+  const int64_t rb = min((int64_t)n * p.group, ra + p.piece);
+  if (ra >= rb) return;
+  const int j = min(sub * 32 + (lane & 31), sinks - 1);
+  frag K[NS], V[NS];
+  {
+    const T* ksrc = (const T*)p.k + (int64_t)(k0 + j) * p.ld_k + (int64_t)hk * p.d;
+    const T* vsrc = (const T*)p.v + (int64_t)(k0 + j) * p.ld_v + (int64_t)hk * p.d;
+#pragma unroll
+    for (int ks = 0; ks < NS; ++ks) {
+      const int e = 16 * ks + 8 * h32;
+      frag z = {};
+      K[ks] = e < p.d ? *reinterpret_cast<const frag*>(ksrc + e) : z;
+      V[ks] = e < p.d ? *reinterpret_cast<const frag*>(vsrc + e) : z;
+    }
+  }
+  uint32_t tr[2];
+  Tile<T, DP>::across_addr(lane, tr);
+  f32x16 dK[ND], dV[ND];
+#pragma unroll
+  for (int dt = 0; dt < ND; ++dt) dK[dt] = dV[dt] = f32x16{};
+  Stage<T, DP, RT, 256> sq, sg;
+  for (int64_t r0 = ra; r0 < rb; r0 += RT) {
+    const int t0 = (int)(r0 / p.group), g0 = (int)(r0 - (int64_t)t0 * p.group);
+    const int cnt = (int)min((int64_t)RT, rb - r0), first = q0 + t0, h0 = hk * p.group;
+    auto at = [&](const void* base, int64_t ld, int r) {
+      const int tg = (g0 + r) / p.group;
+      return (const T*)base + (int64_t)(first + tg) * ld + (int64_t)(h0 + g0 + r - tg * p.group) * p.d;
+    };
+    sq.load(tid, cnt, p.d, [&](int r) { return at(p.q, p.ld_q, r); });
+    sg.load(tid, cnt, p.d, [&](int r) { return at(p.dout, p.ld_dout, r); });
+    float lse2 = INFINITY, delta = 0.f;                    // a row past the end has weight 0
+    if (tid < cnt) {
+      const int tg = (g0 + tid) / p.group, head = h0 + g0 + tid - tg * p.group;
+      lse2 = p.lse[(int64_t)head * p.ld_lse + first + tg] * kLog2e;
+      delta = p.delta[(int64_t)head * p.sum_q + first + tg];
+    }
+    __syncthreads();
+    sq.store(tid, sh.t.q);
+    sg.store(tid, sh.t.g);
+    if (tid < RT) {
+      sh.t.lse[tid] = lse2;
+      sh.t.delta[tid] = delta;
+    }
+    __syncthreads();
+    const int rw = 32 * wave;
+    if (rw >= cnt) continue;
+    f32x16 S = f32x16{}, dP = f32x16{};
+#pragma unroll
+    for (int ks = 0; ks < NS; ++ks) {
+      S = mma32(Tile<T, DP>::along(sh.t.q, rw, ks, lane), K[ks], S);
+      dP = mma32(Tile<T, DP>::along(sh.t.g, rw, ks, lane), V[ks], dP);
+    }
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+      const int r = rw + 8 * e4 + 4 * h32;
+      const f32x4 ls = *reinterpret_cast<const f32x4*>(sh.t.lse + r), de = *reinterpret_cast<const f32x4*>(sh.t.delta + r);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float w = __builtin_amdgcn_exp2f(fmaf(S[4 * e4 + u], p.c, -ls[u]));
+        S[4 * e4 + u] = w;
+        dP[4 * e4 + u] = w * (dP[4 * e4 + u] - de[u]);
+      }
+    }
+#pragma unroll
+    for (int nn = 0; nn < 2; ++nn) {
+      frag W, D;
+      to_operand(S, nn, W);
+      to_operand(dP, nn, D);
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) {
+        dV[dt] = mma32(across<DP>(sh.t.g, rw + 16 * nn, dt, lane, tr), W, dV[dt]);
+        dK[dt] = mma32(across<DP>(sh.t.q, rw + 16 * nn, dt, lane, tr), D, dK[dt]);
+      }
+    }
+  }
+  float* out = p.sink_part + ((((int64_t)i * p.kv_heads + hk) * p.subs + sub) * p.pieces + piece) * 64 * DP;
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {                            // dK, then dV
+    __syncthreads();
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const f32x16& a = x ? dV[dt] : dK[dt];
+        *reinterpret_cast<f32x4*>(&sh.sum[wave][(lane & 31) * DP + 32 * dt + 2 * e + 4 * h32]) =
+            f32x4{a[e], a[e + 1], a[e + 2], a[e + 3]};
+      }
+    __syncthreads();
+    for (int u = tid * 4; u < 32 * DP; u += 1024) {
+      f32x4 a = *reinterpret_cast<f32x4*>(&sh.sum[0][u]);
+#pragma unroll
+      for (int w = 1; w < 4; ++w) a += *reinterpret_cast<f32x4*>(&sh.sum[w][u]);
+      *reinterpret_cast<f32x4*>(out + x * 32 * DP + u) = a;
+    }
+  }
+}
+
+// The pieces' sums, added in order.
+template <int DP>
+__global__ void __launch_bounds__(256)
+sink_sum_kernel(WindowBwdParams p) {
+  const int64_t item = block_id();
+  if (item >= p.items) return;
+  constexpr int kParts = 64 * DP / 1024;                   // workgroups per block of sinks
+  const int part = (int)(item % kParts);
+  const int64_t blk = item / kParts;
+  const int sub = (int)(blk % p.subs), i = (int)(blk / p.subs / p.kv_heads);
+  const int n = p.cu_q[i + 1] - p.cu_q[i], m = p.cu_k[i + 1] - p.cu_k[i], off = m - n;
+  if (sub * 32 >= min(p.sinks, m)) return;
+  const int jb = sub * 32 & ~127, jl = min(jb + 127, m - 1);
+  const int ta = p.right >= 0 ? min(max(0, jb - p.right - off), n) : 0;
+  const int64_t rows = (int64_t)(n - max(ta, window_end(jl, p.left, off, n))) * p.group;
+  const int pieces = (int)((rows + p.piece - 1) / p.piece);
+  const float* src = p.sink_part + blk * p.pieces * 64 * DP + part * 1024 + threadIdx.x * 4;
+  f32x4 a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int x = 0; x < pieces; ++x) a += *reinterpret_cast<const f32x4*>(src + (int64_t)x * 64 * DP);
+  if (pieces > 0) *reinterpret_cast<f32x4*>(p.sink_sum + blk * 64 * DP + part * 1024 + threadIdx.x * 4) = a;
+}
+
+// How the sinks' part past the window is cut: pieces of at least kSinkPiece rows,
+// fewer and longer ones where there are many blocks of sinks, so that the partial
+// sums stay bounded.
+constexpr int kSinkPiece = 512, kSinkItems = 1024;
+struct SinkPlan {
+  int split, subs, pieces, piece, dp;
+  size_t delta_bytes, part_bytes, sum_bytes;
+};
+SinkPlan sink_plan(const nt_window_args& a) {
+  SinkPlan s{};
+  const nt_layout &Lq = *a.q_layout, &Lk = *a.kv_layout;
+  s.delta_bytes = ((size_t)a.heads * Lq.sum_n * sizeof(float) + 15) / 16 * 16;
+  s.dp = a.head_dim <= 32 ? 32 : a.head_dim <= 64 ? 64 : 128;
+  if (a.left < 0 || a.sinks == 0) return s;
+  int64_t rows = 0;                                        // most rows past the window of the first keys
+  for (int i = 0; i < Lq.batch; ++i) {
+    const int64_t n = Lq.lengths[i], m = Lk.lengths[i];
+    if (m == 0) continue;
+    const int64_t end = (m < 128 ? m : 128) - 1 + a.left - (m - n) + 1;
+    rows = std::max(rows, (n - std::max<int64_t>(0, std::min(n, end))) * (a.heads / a.kv_heads));
+  }
+  if (rows <= kSinkPiece) return s;
+  s.split = 1;
+  s.subs = (a.sinks + 31) / 32;
+  const int64_t blocks = (int64_t)Lq.batch * a.kv_heads * s.subs;
+  const int64_t want = std::max<int64_t>(1, std::min(rows / kSinkPiece, kSinkItems / blocks));
+  s.piece = (int)((rows + want - 1) / want + 127) / 128 * 128;
+  s.pieces = (int)((rows + s.piece - 1) / s.piece);
+  s.part_bytes = (size_t)blocks * s.pieces * 64 * s.dp * sizeof(float);
+  s.sum_bytes = (size_t)blocks * 64 * s.dp * sizeof(float);
+  return s;
+}
+
 template <typename T, int DP>
 hipError_t launch_backward(WindowBwdParams p, int64_t q_items, int64_t k_items, hipStream_t s) {
   p.items = q_items;
   if (q_items > 0) window_dq_kernel<T, DP><<<folded_grid(q_items), 256, 0, s>>>(p);
   if (hipError_t e = hipGetLastError()) return e;
+  if (p.split) {
+    p.items = (int64_t)p.batch * p.kv_heads * p.subs * p.pieces;
+    window_sink_kernel<T, DP><<<folded_grid(p.items), 256, 0, s>>>(p);
+    if (hipError_t e = hipGetLastError()) return e;
+    p.items = (int64_t)p.batch * p.kv_heads * p.subs * (64 * DP / 1024);
+    sink_sum_kernel<DP><<<folded_grid(p.items), 256, 0, s>>>(p);
+    if (hipError_t e = hipGetLastError()) return e;
+  }
   p.items = k_items;
   if (k_items > 0) window_dkv_kernel<T, DP><<<folded_grid(k_items), 256, 0, s>>>(p);
   return hipGetLastError();
@@ -308,11 +524,12 @@ hipError_t launch_backward(WindowBwdParams p, int64_t q_items, int64_t k_items, 
 }  // namespace
 
 size_t window_backward_workspace_bytes(const nt_window_args& a) {
-  return ((size_t)a.heads * a.q_layout->sum_n * sizeof(float) + 15) / 16 * 16;
+  const SinkPlan s = sink_plan(a);
+  return s.delta_bytes + s.part_bytes + s.sum_bytes;
 }
 
 hipError_t launch_window_backward(const nt_window_args& a, hipStream_t s) {
-  const nt_layout &Lq = *a.q_layout, &Lk = a.kv_layout ? *a.kv_layout : Lq;
+  const nt_layout &Lq = *a.q_layout, &Lk = *a.kv_layout;
   WindowBwdParams p{};
   p.cu_q = Lq.d_cu_seqlens;
   p.cu_k = Lk.d_cu_seqlens;
@@ -333,6 +550,13 @@ hipError_t launch_window_backward(const nt_window_args& a, hipStream_t s) {
   p.lse = a.lse;
   p.delta = (float*)a.workspace;
   p.sum_q = Lq.sum_n;
+  const SinkPlan sp = sink_plan(a);
+  p.split = sp.split;
+  p.subs = sp.subs;
+  p.pieces = sp.pieces;
+  p.piece = sp.piece;
+  p.sink_part = (float*)((char*)a.workspace + sp.delta_bytes);
+  p.sink_sum = (float*)((char*)a.workspace + sp.delta_bytes + sp.part_bytes);
   const int64_t qi = Lq.sum_n ? win::block_count(Lq.sum_n, Lq.batch, p.group, kBlockShift) * p.kv_heads : 0;
   const int64_t ki = Lk.sum_n ? win::block_count(Lk.sum_n, Lk.batch, 1, kBlockShift) * p.kv_heads : 0;
   const bool bf = a.dtype == NT_BF16;

@@ -109,6 +109,7 @@ def test_heads(dtype, H, K):
     ([200], [200], 3, 0, 199), ([200], [200], 3, 0, 500),
     ([257], [257], 64, 0, 4), ([257], [257], 63, 1, 0),
     ([130], [700], 100, 0, 5), ([130], [700], 600, 0, 65), ([20], [300], 10, 3, 2),
+    ([900, 0, 40], [900, 7, 700], 20, 0, 3), ([800], [850], 9, 4, 200),   # sinks seen far past their window
     ([150], [150], -1, 5, 3), ([150], [150], 5, -1, 3),
 ])
 def test_edges(dtype, n, m, left, right, sinks):
