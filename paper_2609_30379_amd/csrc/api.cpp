@@ -792,6 +792,7 @@ nt_status window_sizes(const nt_window_args* a, nt_window_args* out) {
   if (!valid_dtype(a->dtype)) return nt::fail(NT_ERR_INVALID_ARG, "bad dtype");
   if (a->heads <= 0 || a->kv_heads <= 0 || a->heads % a->kv_heads)
     return nt::fail(NT_ERR_INVALID_ARG, "heads must be a positive multiple of kv_heads");
+  if (a->heads > 65536) return nt::fail(NT_ERR_UNSUPPORTED, "window attention supports at most 65536 heads");
   if (a->head_dim <= 0) return nt::fail(NT_ERR_INVALID_ARG, "head_dim must be > 0");
   if (a->head_dim % 8 || a->head_dim > 128)
     return nt::fail(NT_ERR_UNSUPPORTED, "window attention supports head_dim in multiples of 8 up to 128");

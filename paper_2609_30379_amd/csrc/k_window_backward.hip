@@ -20,6 +20,7 @@ struct WindowBwdParams {
   const int32_t *cu_q, *cu_k;
   int batch, heads, kv_heads, group, d, left, right, sinks;
   float scale, c;                // c = scale * log2(e)
+  float inv_group;
   const void *q, *k, *v, *o, *dout;
   void *dq, *dk, *dv;
   int64_t ld_q, ld_k, ld_v, ld_o, ld_dout, ld_dq, ld_dk, ld_dv, ld_lse;
@@ -57,7 +58,7 @@ window_dq_kernel(WindowBwdParams p) {
   if (r0 >= rows) return;
   const int t0 = (int)(r0 / p.group), g0 = (int)(r0 - (int64_t)t0 * p.group);
   const int last = (int)min((int64_t)127, rows - 1 - r0), off = m - n;
-  const int x = min(wave * 32 + (lane & 31), last), tg = (g0 + x) / p.group;
+  const int x = min(wave * 32 + (lane & 31), last), tg = div_group(g0 + x, p.inv_group);
   const int t = t0 + tg, g = g0 + x - tg * p.group, pos = off + t, head = hk * p.group + g;
   const int lo = p.left >= 0 ? pos - p.left : 0, hi = p.right >= 0 ? min(pos + p.right, m - 1) : m - 1;
   const bool live = wave * 32 <= last, mine = wave * 32 + (lane & 31) <= last;
@@ -207,25 +208,35 @@ window_dkv_kernel(WindowBwdParams p) {
   Stage<T, DP, RT, 256> sq, sg;
   float r_lse = 0.f, r_delta = 0.f;
   int r_pos = 0;
-  auto load = [&](int tile) {
-    const int64_t r0 = ra + (int64_t)tile * RT;
-    const int t0 = (int)(r0 / p.group), g0 = (int)(r0 - (int64_t)t0 * p.group);
-    const int cnt = (int)min((int64_t)RT, rb - r0);
-    const int first = q0 + t0, h0 = hk * p.group;
+  // the tile's first row as (t0, g0), moved on by RT rows per tile
+  const int step_t = RT / p.group, step_g = RT - step_t * p.group;
+  int lt0 = ta, lg0 = 0;
+  int64_t left_rows = rb - ra;
+  auto load = [&]() {
+    const int cnt = (int)min((int64_t)RT, left_rows);
+    const int first = q0 + lt0, h0 = hk * p.group;
     auto at = [&](const void* base, int64_t ld, int r) {
-      const int tg = (g0 + r) / p.group;
-      return (const T*)base + (int64_t)(first + tg) * ld + (int64_t)(h0 + g0 + r - tg * p.group) * p.d;
+      const int tg = div_group(lg0 + r, p.inv_group);
+      return (const T*)base + (int64_t)(first + tg) * ld + (int64_t)(h0 + lg0 + r - tg * p.group) * p.d;
     };
     sq.load(tid, cnt, p.d, [&](int r) { return at(p.q, p.ld_q, r); });
     sg.load(tid, cnt, p.d, [&](int r) { return at(p.dout, p.ld_dout, r); });
     if (tid < RT) {
-      const int r = min(tid, cnt - 1), tg = (g0 + r) / p.group, head = h0 + g0 + r - tg * p.group;
+      const int r = min(tid, cnt - 1), tg = div_group(lg0 + r, p.inv_group), head = h0 + lg0 + r - tg * p.group;
       r_lse = p.lse[(int64_t)head * p.ld_lse + first + tg] * kLog2e;
       r_delta = p.delta[(int64_t)head * p.sum_q + first + tg];
-      r_pos = tid < cnt ? off + t0 + tg : INT32_MIN;            // no key sees a row past the end
+      r_pos = tid < cnt ? off + lt0 + tg : INT32_MIN;           // no key sees a row past the end
+    }
+    left_rows -= RT;
+    lt0 += step_t;
+    lg0 += step_g;
+    if (lg0 >= p.group) {
+      lg0 -= p.group;
+      ++lt0;
     }
   };
-  if (tiles > 0) load(0);
+  int nt0 = ta, ng0 = 0;                                        // the tile that is worked on next
+  if (tiles > 0) load();
   for (int tile = 0; tile < tiles; ++tile) {
     __syncthreads();
     sq.store(tid, Qs);
@@ -236,12 +247,15 @@ window_dkv_kernel(WindowBwdParams p) {
       pos_s[tid] = r_pos;
     }
     __syncthreads();
-    const int64_t r0 = ra + (int64_t)tile * RT;
-    if (tile + 1 < tiles) load(tile + 1);
+    const int ct0 = nt0, cg0 = ng0;
+    const int64_t cur_rows = rb - ra - (int64_t)tile * RT;
+    nt0 = lt0;
+    ng0 = lg0;
+    const int pa = off + ct0, pe = off + ct0 + div_group(cg0 + (int)min((int64_t)RT, cur_rows) - 1, p.inv_group);
+    if (tile + 1 < tiles) load();
     if (!live) continue;
-    const int pa = off + (int)(r0 / p.group), pe = off + (int)((min(r0 + RT, rb) - 1) / p.group);
     if (!__any(pe >= plo && pa <= phi)) continue;
-    const bool whole = __all(r0 + RT <= rb && pa >= plo && pe <= phi);
+    const bool whole = __all(cur_rows >= RT && pa >= plo && pe <= phi);
 #pragma unroll
     for (int rbk = 0; rbk < RB; ++rbk) {
       f32x16 S = f32x16{}, dP = f32x16{};
@@ -375,14 +389,14 @@ window_sink_kernel(WindowBwdParams p) {
     const int t0 = (int)(r0 / p.group), g0 = (int)(r0 - (int64_t)t0 * p.group);
     const int cnt = (int)min((int64_t)RT, rb - r0), first = q0 + t0, h0 = hk * p.group;
     auto at = [&](const void* base, int64_t ld, int r) {
-      const int tg = (g0 + r) / p.group;
+      const int tg = div_group(g0 + r, p.inv_group);
       return (const T*)base + (int64_t)(first + tg) * ld + (int64_t)(h0 + g0 + r - tg * p.group) * p.d;
     };
     sq.load(tid, cnt, p.d, [&](int r) { return at(p.q, p.ld_q, r); });
     sg.load(tid, cnt, p.d, [&](int r) { return at(p.dout, p.ld_dout, r); });
     float lse2 = INFINITY, delta = 0.f;                    // a row past the end has weight 0
     if (tid < cnt) {
-      const int tg = (g0 + tid) / p.group, head = h0 + g0 + tid - tg * p.group;
+      const int tg = div_group(g0 + tid, p.inv_group), head = h0 + g0 + tid - tg * p.group;
       lse2 = p.lse[(int64_t)head * p.ld_lse + first + tg] * kLog2e;
       delta = p.delta[(int64_t)head * p.sum_q + first + tg];
     }
@@ -542,6 +556,7 @@ hipError_t launch_window_backward(const nt_window_args& a, hipStream_t s) {
   p.right = a.right;
   p.sinks = a.sinks;
   p.scale = a.scale;
+  p.inv_group = 1.f / (float)p.group;
   p.c = a.scale * win::kLog2e;
   p.q = a.q; p.k = a.k; p.v = a.v; p.o = a.o; p.dout = a.dout;
   p.dq = a.dq; p.dk = a.dk; p.dv = a.dv;

@@ -157,6 +157,10 @@ template <typename T, int DP, int ROWS, int THREADS> struct Stage {
   }
 };
 
+// x / group for 0 <= x < 2^20: the quotient of x + 1/2 stays at least 1 / (2 group)
+// away from a whole number, far more than the product's rounding.
+__device__ __forceinline__ int div_group(int x, float inv_group) { return (int)(((float)x + 0.5f) * inv_group); }
+
 // Sum over the two lanes l, l ^ 32 that hold one column of an accumulator.
 __device__ __forceinline__ float pair_sum(float v) {
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);

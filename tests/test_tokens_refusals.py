@@ -47,6 +47,7 @@ WINDOW = [
     (dict(heads=0), B.NT_ERR_INVALID_ARG, "heads"),
     (dict(heads=3), B.NT_ERR_INVALID_ARG, "heads"),
     (dict(kv_heads=0), B.NT_ERR_INVALID_ARG, "heads"),
+    (dict(heads=1 << 17), B.NT_ERR_UNSUPPORTED, "heads"),
     (dict(head_dim=0), B.NT_ERR_INVALID_ARG, "head_dim"),
     (dict(head_dim=36), B.NT_ERR_UNSUPPORTED, "head_dim"),
     (dict(head_dim=136), B.NT_ERR_UNSUPPORTED, "head_dim"),
