@@ -9,6 +9,7 @@
 // the products, so P and dS go from accumulators into the next operand in
 // registers.
 #include <algorithm>
+#include <type_traits>
 
 #include "window_device.h"
 
@@ -19,7 +20,7 @@ using namespace win;
 struct WindowBwdParams {
   const int32_t *cu_q, *cu_k;
   int batch, heads, kv_heads, group, d, left, right, sinks;
-  float scale, c;                // c = scale * log2(e)
+  float scale, c, qmul;          // c = |scale| log2(e) (1 for scale 0); qmul: 1, -1 or 0, what one operand of q . k is multiplied by
   float inv_group;
   const void *q, *k, *v, *o, *dout;
   void *dq, *dk, *dv;
@@ -28,6 +29,7 @@ struct WindowBwdParams {
   float* delta;                  // [heads][sum N] workspace
   int64_t sum_q;
   int64_t items;
+  bool narrow;
   // gradients of the sinks from the queries past their window (window_sink_kernel)
   int split;                     // done apart, in pieces of `piece` rows
   int subs, pieces, piece;       // blocks of 32 sinks, most pieces of a sample, rows per piece
@@ -41,13 +43,13 @@ __device__ __forceinline__ int window_end(int jl, int left, int off, int n) { re
 constexpr int kBlockShift = 7;
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(256, DP == 32 ? 3 : DP == 128 && sizeof(T) == 4 ? 1 : 2)
+__global__ void __launch_bounds__(256, DP == 32 ? 3 : DP == 128 ? 1 : 2)
 window_dq_kernel(WindowBwdParams p) {
   typedef typename Frag<T>::type frag;
   constexpr int KT = sizeof(T) == 2 ? 64 : 32, KB = KT / 32, NS = DP / 16, ND = DP / 32;
-  __shared__ __attribute__((aligned(16))) T Ks[KT * Tile<T, DP>::kLd];
-  __shared__ __attribute__((aligned(16))) T Vs[KT * Tile<T, DP>::kLd];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h32 = lane >> 5;
+  __shared__ __attribute__((aligned(16))) T Kb[2][KT * Tile<T, DP>::kLd];
+  __shared__ __attribute__((aligned(16))) T Vb[2][KT * Tile<T, DP>::kLd];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h32 = lane >> 5;
   const int64_t item = block_id();
   if (item >= p.items) return;
   const int hk = (int)(item % p.kv_heads);
@@ -61,6 +63,9 @@ window_dq_kernel(WindowBwdParams p) {
   const int x = min(wave * 32 + (lane & 31), last), tg = div_group(g0 + x, p.inv_group);
   const int t = t0 + tg, g = g0 + x - tg * p.group, pos = off + t, head = hk * p.group + g;
   const int lo = p.left >= 0 ? pos - p.left : 0, hi = p.right >= 0 ? min(pos + p.right, m - 1) : m - 1;
+  const int pos_a = off + t0 + (g0 + min(wave * 32, last)) / p.group, pos_b = off + t0 + (g0 + min(wave * 32 + 31, last)) / p.group;
+  const int lo_a = p.left >= 0 ? pos_a - p.left : 0, hi_a = p.right >= 0 ? min(pos_a + p.right, m - 1) : m - 1;
+  const int lo_b = p.left >= 0 ? pos_b - p.left : 0, hi_b = p.right >= 0 ? min(pos_b + p.right, m - 1) : m - 1;
   const bool live = wave * 32 <= last, mine = wave * 32 + (lane & 31) <= last;
 
   frag Q[NS], G[NS];
@@ -80,8 +85,9 @@ window_dq_kernel(WindowBwdParams p) {
       for (int u = 0; u < 8; ++u) delta = fmaf((float)o[u], (float)G[ks][u], delta);
     }
     delta = pair_sum(delta);
+    multiply<T>(Q, p.qmul);
   }
-  const float lse2 = p.lse[(int64_t)head * p.ld_lse + q0 + t] * kLog2e;
+  const float lse = p.lse[(int64_t)head * p.ld_lse + q0 + t], nlse2 = lse == -INFINITY ? 0.f : -lse * kLog2e;
   if (mine && h32 == 0) p.delta[(int64_t)head * p.sum_q + q0 + t] = delta;
   uint32_t tr[2];
   Tile<T, DP>::across_addr(lane, tr);
@@ -95,47 +101,66 @@ window_dq_kernel(WindowBwdParams p) {
   const T* vbase = (const T*)p.v + (int64_t)hk * p.d;
   Stage<T, DP, KT, 256> sk, sv;
   auto load = [&](int tile) {
-    const int j0 = kt.first(tile, KT), cnt = kt.end(tile) - j0;
-    sk.load(tid, cnt, p.d, [&](int r) { return kbase + (int64_t)(k0 + j0 + r) * p.ld_k; });
-    sv.load(tid, cnt, p.d, [&](int r) { return vbase + (int64_t)(k0 + j0 + r) * p.ld_v; });
+    const int j0 = kt.first(tile, KT), cnt = min(kt.end(tile) - j0, KT);
+    sk.load(tid, kbase + (int64_t)(k0 + j0) * p.ld_k, p.ld_k, cnt, p.d, p.narrow);
+    sv.load(tid, vbase + (int64_t)(k0 + j0) * p.ld_v, p.ld_v, cnt, p.d, p.narrow);
   };
-  if (kt.n > 0) load(0);
+  if (kt.n > 0) {
+    load(0);
+    sk.store(tid, Kb[0]);
+    sv.store(tid, Vb[0]);
+  }
   for (int tile = 0; tile < kt.n; ++tile) {
     __syncthreads();
-    sk.store(tid, Ks);
-    sv.store(tid, Vs);
-    __syncthreads();
-    const int j0 = kt.first(tile, KT), jend = kt.end(tile);
+    const T *Ks = Kb[tile & 1], *Vs = Vb[tile & 1];
     if (tile + 1 < kt.n) load(tile + 1);
-    if (!live) continue;
-    const int je = min(j0 + KT, jend);
-    if (!__any(j0 <= hi && (je > lo || j0 < p.sinks))) continue;
-    const bool whole = __all(j0 + KT <= jend && j0 + KT - 1 <= hi && (j0 >= lo || j0 + KT <= p.sinks));
+    const int j0 = kt.first(tile, KT), jend = kt.end(tile);
+    if (live && j0 <= hi_b && (min(j0 + KT, jend) > lo_a || j0 < p.sinks)) {
+    const bool whole = j0 + KT <= jend && j0 + KT - 1 <= hi_a && (j0 >= lo_b || j0 + KT <= p.sinks);
+    // Block by block of 32 keys, the reads of a step before the products of the
+    // one before; a hidden pair's score starts from -inf, dP from -D.
+    frag A[NS], B[NS], X[ND], Y[ND];
+    read_along<DP>(Ks, 0, lane, A);
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-      f32x16 S = f32x16{}, dP = f32x16{};
+      f32x16 S = f32x16{}, dP;
+      if (!whole) {
 #pragma unroll
-      for (int ks = 0; ks < NS; ++ks) {
-        S = mma32(Tile<T, DP>::along(Ks, 32 * kb, ks, lane), Q[ks], S);
-        dP = mma32(Tile<T, DP>::along(Vs, 32 * kb, ks, lane), G[ks], dP);
-      }
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        float ds = __builtin_amdgcn_exp2f(fmaf(S[e], p.c, -lse2)) * (dP[e] - delta);
-        if (!whole) {
+        for (int e = 0; e < 16; ++e) {
           const int j = j0 + 32 * kb + 8 * (e >> 2) + 4 * h32 + (e & 3);
-          ds = j < jend && j <= hi && (j >= lo || j < p.sinks) ? ds : 0.f;
+          S[e] = j < jend && j <= hi && (j >= lo || j < p.sinks) ? 0.f : -INFINITY;
         }
-        S[e] = ds;
       }
 #pragma unroll
-      for (int nn = 0; nn < 2; ++nn) {
-        frag D;
-        to_operand(S, nn, D);
+      for (int e = 0; e < 16; ++e) dP[e] = -delta;
+      pin();
+      read_along<DP>(Vs, 32 * kb, lane, B);
+      pin();
+      S = product(A, Q, S);
+      pin();
+      read_across<DP>(Ks, 32 * kb, lane, tr, X);
+      pin();
+      dP = product(B, G, dP);
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt)
-          dQ[dt] = mma32(across<DP>(Ks, 32 * kb + 16 * nn, dt, lane, tr), D, dQ[dt]);
-      }
+      for (int e = 0; e < 16; ++e) S[e] = __builtin_amdgcn_exp2f(fmaf(S[e], p.c, nlse2));
+      pin();
+      read_across<DP>(Ks, 32 * kb + 16, lane, tr, Y);
+      pin();
+#pragma unroll
+      for (int e = 0; e < 16; ++e) S[e] *= dP[e];
+      frag D;
+      to_operand(S, 0, D);
+      add_products(X, D, dQ);
+      to_operand(S, 1, D);
+      pin();
+      if (kb + 1 < KB) read_along<DP>(Ks, 32 * kb + 32, lane, A);
+      pin();
+      add_products(Y, D, dQ);
+    }
+    }
+    if (tile + 1 < kt.n) {
+      sk.store(tid, Kb[~tile & 1]);
+      sv.store(tid, Vb[~tile & 1]);
     }
   }
   if (!mine) return;
@@ -156,16 +181,16 @@ window_dq_kernel(WindowBwdParams p) {
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(256, DP == 128 ? 1 : 2)
+__global__ void __launch_bounds__(256, DP == 128 || (DP == 64 && sizeof(T) == 4) ? 1 : 2)
 window_dkv_kernel(WindowBwdParams p) {
   typedef typename Frag<T>::type frag;
   constexpr int RT = sizeof(T) == 2 ? 64 : 32, RB = RT / 32, NS = DP / 16, ND = DP / 32;
-  __shared__ __attribute__((aligned(16))) T Qs[RT * Tile<T, DP>::kLd];
-  __shared__ __attribute__((aligned(16))) T Gs[RT * Tile<T, DP>::kLd];
-  __shared__ __attribute__((aligned(16))) float lse_s[RT];
-  __shared__ __attribute__((aligned(16))) float delta_s[RT];
-  __shared__ __attribute__((aligned(16))) int pos_s[RT];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h32 = lane >> 5;
+  __shared__ __attribute__((aligned(16))) T Qb[2][RT * Tile<T, DP>::kLd];
+  __shared__ __attribute__((aligned(16))) T Gb[2][RT * Tile<T, DP>::kLd];
+  __shared__ __attribute__((aligned(16))) float lse_b[2][RT];
+  __shared__ __attribute__((aligned(16))) float delta_b[2][RT];
+  __shared__ __attribute__((aligned(16))) int pos_b[2][RT];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h32 = lane >> 5;
   const int64_t item = block_id();
   if (item >= p.items) return;
   const int hk = (int)(item % p.kv_heads);
@@ -182,6 +207,12 @@ window_dkv_kernel(WindowBwdParams p) {
   const int plo = p.right >= 0 ? j - p.right : INT32_MIN + 1;
   const int phi = p.left >= 0 && j >= p.sinks ? j + p.left : INT32_MAX;
 
+  // the same bounds over the wave's keys
+  const int ja = min(jb + wave * 32, m - 1), je = min(jb + wave * 32 + 31, m - 1);
+  const int plo_a = p.right >= 0 ? ja - p.right : INT32_MIN + 1, plo_b = p.right >= 0 ? je - p.right : INT32_MIN + 1;
+  const int phi_a = p.left >= 0 && je >= p.sinks ? max(ja, p.sinks) + p.left : INT32_MAX;
+  const int phi_b = p.left >= 0 && ja >= p.sinks ? je + p.left : INT32_MAX;
+
   frag K[NS], V[NS];
   {
     const T* ksrc = (const T*)p.k + (int64_t)(k0 + j) * p.ld_k + (int64_t)hk * p.d;
@@ -193,6 +224,7 @@ window_dkv_kernel(WindowBwdParams p) {
       K[ks] = e < p.d ? *reinterpret_cast<const frag*>(ksrc + e) : z;
       V[ks] = e < p.d ? *reinterpret_cast<const frag*>(vsrc + e) : z;
     }
+    multiply<T>(K, p.qmul);
   }
   uint32_t tr[2];
   Tile<T, DP>::across_addr(lane, tr);
@@ -213,17 +245,15 @@ window_dkv_kernel(WindowBwdParams p) {
   int lt0 = ta, lg0 = 0;
   int64_t left_rows = rb - ra;
   auto load = [&]() {
-    const int cnt = (int)min((int64_t)RT, left_rows);
+    const int cnt = (int)min((int64_t)RT, left_rows), queries = min(tb - lt0, RT + 1);
     const int first = q0 + lt0, h0 = hk * p.group;
-    auto at = [&](const void* base, int64_t ld, int r) {
-      const int tg = div_group(lg0 + r, p.inv_group);
-      return (const T*)base + (int64_t)(first + tg) * ld + (int64_t)(h0 + lg0 + r - tg * p.group) * p.d;
-    };
-    sq.load(tid, cnt, p.d, [&](int r) { return at(p.q, p.ld_q, r); });
-    sg.load(tid, cnt, p.d, [&](int r) { return at(p.dout, p.ld_dout, r); });
+    sq.load_group(tid, (const T*)p.q + (int64_t)first * p.ld_q + (int64_t)h0 * p.d, p.ld_q, queries, lg0, p.group,
+                  p.inv_group, p.d, p.narrow);
+    sg.load_group(tid, (const T*)p.dout + (int64_t)first * p.ld_dout + (int64_t)h0 * p.d, p.ld_dout, queries, lg0,
+                  p.group, p.inv_group, p.d, p.narrow);
     if (tid < RT) {
       const int r = min(tid, cnt - 1), tg = div_group(lg0 + r, p.inv_group), head = h0 + lg0 + r - tg * p.group;
-      r_lse = p.lse[(int64_t)head * p.ld_lse + first + tg] * kLog2e;
+      r_lse = p.lse[(int64_t)head * p.ld_lse + first + tg];
       r_delta = p.delta[(int64_t)head * p.sum_q + first + tg];
       r_pos = tid < cnt ? off + lt0 + tg : INT32_MIN;           // no key sees a row past the end
     }
@@ -235,67 +265,97 @@ window_dkv_kernel(WindowBwdParams p) {
       ++lt0;
     }
   };
+  auto store = [&](int buf) {
+    sq.store(tid, Qb[buf]);
+    sg.store(tid, Gb[buf]);
+    if (tid < RT) {
+      lse_b[buf][tid] = r_lse == -INFINITY ? 0.f : r_lse * -kLog2e;   // -inf: a row that sees nothing
+      delta_b[buf][tid] = -r_delta;
+      pos_b[buf][tid] = r_pos;
+    }
+  };
   int nt0 = ta, ng0 = 0;                                        // the tile that is worked on next
-  if (tiles > 0) load();
+  if (tiles > 0) {
+    load();
+    store(0);
+  }
   for (int tile = 0; tile < tiles; ++tile) {
     __syncthreads();
-    sq.store(tid, Qs);
-    sg.store(tid, Gs);
-    if (tid < RT) {
-      lse_s[tid] = r_lse;
-      delta_s[tid] = r_delta;
-      pos_s[tid] = r_pos;
-    }
-    __syncthreads();
-    const int ct0 = nt0, cg0 = ng0;
-    const int64_t cur_rows = rb - ra - (int64_t)tile * RT;
+    const T *Qs = Qb[tile & 1], *Gs = Gb[tile & 1];
+    const float *lse_s = lse_b[tile & 1], *delta_s = delta_b[tile & 1];
+    const int* pos_s = pos_b[tile & 1];
+    const int cur_rows = (int)min((int64_t)RT, rb - ra - (int64_t)tile * RT);
+    const int pa = off + nt0, pe = off + nt0 + (ng0 + cur_rows - 1) / p.group;
     nt0 = lt0;
     ng0 = lg0;
-    const int pa = off + ct0, pe = off + ct0 + div_group(cg0 + (int)min((int64_t)RT, cur_rows) - 1, p.inv_group);
     if (tile + 1 < tiles) load();
-    if (!live) continue;
-    if (!__any(pe >= plo && pa <= phi)) continue;
-    const bool whole = __all(cur_rows >= RT && pa >= plo && pe <= phi);
+    if (live && pe >= plo_a && pa <= phi_b) {
+    const bool whole = cur_rows == RT && pa >= plo_b && pe <= phi_a;
+    // One 32-row block after the other; each step issues the reads of the next
+    // one before its products, and the exponentials and score gradients run
+    // under products.  A hidden pair's score starts from -inf, so its weight is 0;
+    // dP starts from -D.
+    frag A[NS], B[NS], X[ND], Y[ND];
+    read_along<DP>(Qs, 0, lane, A);
 #pragma unroll
     for (int rbk = 0; rbk < RB; ++rbk) {
-      f32x16 S = f32x16{}, dP = f32x16{};
+      const int r0 = 32 * rbk;
+      f32x16 S = f32x16{}, dP;
+      if (!whole) {
 #pragma unroll
-      for (int ks = 0; ks < NS; ++ks) {
-        S = mma32(Tile<T, DP>::along(Qs, 32 * rbk, ks, lane), K[ks], S);
-        dP = mma32(Tile<T, DP>::along(Gs, 32 * rbk, ks, lane), V[ks], dP);
+        for (int e4 = 0; e4 < 4; ++e4) {
+          const int4 ps = *reinterpret_cast<const int4*>(pos_s + r0 + 8 * e4 + 4 * h32);
+          const int pr[4] = {ps.x, ps.y, ps.z, ps.w};
+#pragma unroll
+          for (int u = 0; u < 4; ++u) S[4 * e4 + u] = pr[u] >= plo && pr[u] <= phi ? 0.f : -INFINITY;
+        }
       }
+      pin();
+      read_along<DP>(Gs, r0, lane, B);
 #pragma unroll
       for (int e4 = 0; e4 < 4; ++e4) {
-        const int r = 32 * rbk + 8 * e4 + 4 * h32;
-        const f32x4 ls = *reinterpret_cast<const f32x4*>(lse_s + r), de = *reinterpret_cast<const f32x4*>(delta_s + r);
-        const int4 ps = *reinterpret_cast<const int4*>(pos_s + r);
-        const int pr[4] = {ps.x, ps.y, ps.z, ps.w};
+        const f32x4 de = *reinterpret_cast<const f32x4*>(delta_s + r0 + 8 * e4 + 4 * h32);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int e = 4 * e4 + u;
-          float w = __builtin_amdgcn_exp2f(fmaf(S[e], p.c, -ls[u]));
-          float ds = w * (dP[e] - de[u]);
-          if (!whole) {
-            const bool seen = pr[u] >= plo && pr[u] <= phi;
-            w = seen ? w : 0.f;
-            ds = seen ? ds : 0.f;
-          }
-          S[e] = w;
-          dP[e] = ds;
-        }
+        for (int u = 0; u < 4; ++u) dP[4 * e4 + u] = de[u];
       }
+      pin();
+      S = product(A, K, S);
+      pin();
+      read_across<DP>(Gs, r0, lane, tr, X);
+      pin();
+      dP = product(B, V, dP);
+      frag W, D;
 #pragma unroll
-      for (int nn = 0; nn < 2; ++nn) {
-        frag W, D;
-        to_operand(S, nn, W);
-        to_operand(dP, nn, D);
+      for (int e4 = 0; e4 < 4; ++e4) {
+        const f32x4 ls = *reinterpret_cast<const f32x4*>(lse_s + r0 + 8 * e4 + 4 * h32);
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt) {
-          dV[dt] = mma32(across<DP>(Gs, 32 * rbk + 16 * nn, dt, lane, tr), W, dV[dt]);
-          dK[dt] = mma32(across<DP>(Qs, 32 * rbk + 16 * nn, dt, lane, tr), D, dK[dt]);
-        }
+        for (int u = 0; u < 4; ++u) S[4 * e4 + u] = __builtin_amdgcn_exp2f(fmaf(S[4 * e4 + u], p.c, ls[u]));
       }
+      to_operand(S, 0, W);
+      pin();
+      read_across<DP>(Gs, r0 + 16, lane, tr, Y);
+      pin();
+      add_products(X, W, dV);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) dP[e] *= S[e];
+      to_operand(S, 1, W);
+      pin();
+      read_across<DP>(Qs, r0, lane, tr, X);
+      pin();
+      add_products(Y, W, dV);
+      to_operand(dP, 0, D);
+      pin();
+      read_across<DP>(Qs, r0 + 16, lane, tr, Y);
+      pin();
+      add_products(X, D, dK);
+      to_operand(dP, 1, D);
+      pin();
+      if (rbk + 1 < RB) read_along<DP>(Qs, r0 + 32, lane, A);
+      pin();
+      add_products(Y, D, dK);
     }
+    }
+    if (tile + 1 < tiles) store(~tile & 1);
   }
   if (!mine) return;
   if (p.split && j < p.sinks && max(ta, tb) < n) {         // what the queries past the window add to a sink
@@ -353,7 +413,7 @@ window_sink_kernel(WindowBwdParams p) {
     float sum[4][32 * DP];
   };
   __shared__ __attribute__((aligned(16))) Shared sh;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h32 = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h32 = lane >> 5;
   const int64_t item = block_id();
   if (item >= p.items) return;
   const int hk = (int)(item % p.kv_heads), piece = (int)(item / p.kv_heads % p.pieces);
@@ -378,6 +438,7 @@ window_sink_kernel(WindowBwdParams p) {
       K[ks] = e < p.d ? *reinterpret_cast<const frag*>(ksrc + e) : z;
       V[ks] = e < p.d ? *reinterpret_cast<const frag*>(vsrc + e) : z;
     }
+    multiply<T>(K, p.qmul);
   }
   uint32_t tr[2];
   Tile<T, DP>::across_addr(lane, tr);
@@ -388,13 +449,12 @@ window_sink_kernel(WindowBwdParams p) {
   for (int64_t r0 = ra; r0 < rb; r0 += RT) {
     const int t0 = (int)(r0 / p.group), g0 = (int)(r0 - (int64_t)t0 * p.group);
     const int cnt = (int)min((int64_t)RT, rb - r0), first = q0 + t0, h0 = hk * p.group;
-    auto at = [&](const void* base, int64_t ld, int r) {
-      const int tg = div_group(g0 + r, p.inv_group);
-      return (const T*)base + (int64_t)(first + tg) * ld + (int64_t)(h0 + g0 + r - tg * p.group) * p.d;
-    };
-    sq.load(tid, cnt, p.d, [&](int r) { return at(p.q, p.ld_q, r); });
-    sg.load(tid, cnt, p.d, [&](int r) { return at(p.dout, p.ld_dout, r); });
-    float lse2 = INFINITY, delta = 0.f;                    // a row past the end has weight 0
+    const int queries = min(n - t0, RT + 1);
+    sq.load_group(tid, (const T*)p.q + (int64_t)first * p.ld_q + (int64_t)h0 * p.d, p.ld_q, queries, g0, p.group,
+                  p.inv_group, p.d, p.narrow);
+    sg.load_group(tid, (const T*)p.dout + (int64_t)first * p.ld_dout + (int64_t)h0 * p.d, p.ld_dout, queries, g0, p.group,
+                  p.inv_group, p.d, p.narrow);
+    float lse2 = INFINITY, delta = 0.f;                    // a row past the piece has weight 0
     if (tid < cnt) {
       const int tg = div_group(g0 + tid, p.inv_group), head = h0 + g0 + tid - tg * p.group;
       lse2 = p.lse[(int64_t)head * p.ld_lse + first + tg] * kLog2e;
@@ -557,7 +617,8 @@ hipError_t launch_window_backward(const nt_window_args& a, hipStream_t s) {
   p.sinks = a.sinks;
   p.scale = a.scale;
   p.inv_group = 1.f / (float)p.group;
-  p.c = a.scale * win::kLog2e;
+  p.c = a.scale == 0.f ? 1.f : fabsf(a.scale) * win::kLog2e;
+  p.qmul = a.scale == 0.f ? 0.f : a.scale < 0.f ? -1.f : 1.f;
   p.q = a.q; p.k = a.k; p.v = a.v; p.o = a.o; p.dout = a.dout;
   p.dq = a.dq; p.dk = a.dk; p.dv = a.dv;
   p.ld_q = a.ld_q; p.ld_k = a.ld_k; p.ld_v = a.ld_v; p.ld_o = a.ld_o; p.ld_dout = a.ld_dout;
@@ -575,6 +636,9 @@ hipError_t launch_window_backward(const nt_window_args& a, hipStream_t s) {
   const int64_t qi = Lq.sum_n ? win::block_count(Lq.sum_n, Lq.batch, p.group, kBlockShift) * p.kv_heads : 0;
   const int64_t ki = Lk.sum_n ? win::block_count(Lk.sum_n, Lk.batch, 1, kBlockShift) * p.kv_heads : 0;
   const bool bf = a.dtype == NT_BF16;
+  const int size = bf ? 2 : 4;
+  p.narrow = win::narrow_stride(a.ld_q, size) && win::narrow_stride(a.ld_dout, size) &&
+             win::narrow_stride(a.ld_k, size) && win::narrow_stride(a.ld_v, size);
   if (p.d <= 32) return bf ? launch_backward<bf16, 32>(p, qi, ki, s) : launch_backward<float, 32>(p, qi, ki, s);
   if (p.d <= 64) return bf ? launch_backward<bf16, 64>(p, qi, ki, s) : launch_backward<float, 64>(p, qi, ki, s);
   return bf ? launch_backward<bf16, 128>(p, qi, ki, s) : launch_backward<float, 128>(p, qi, ki, s);

@@ -16,6 +16,7 @@
 namespace nt {
 namespace win {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -75,8 +76,8 @@ template <int DP> struct Tile<bf16, DP> {
     if (DP == 64) return ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
     return (r & 3) << 2 | ((r >> 2) & 3);
   }
-  static __device__ __forceinline__ void put(bf16* s, int r, int c, const uint4& v) {
-    *reinterpret_cast<uint4*>(s + r * DP + ((c ^ f(r)) << 3)) = v;
+  static __device__ __forceinline__ void put(bf16* s, int r, int c, const u32x4& v) {
+    *reinterpret_cast<u32x4*>(s + r * DP + ((c ^ f(r)) << 3)) = v;
   }
   // row base + l % 32, elements 16 ks + 8 (l / 32) ..
   static __device__ __forceinline__ bf16x8 along(const bf16* s, int base, int ks, int lane) {
@@ -102,8 +103,8 @@ template <int DP> struct Tile<bf16, DP> {
 template <int DP> struct Tile<float, DP> {
   static constexpr int kLd = DP + 4;
   static constexpr int kPieces = DP / 4;
-  static __device__ __forceinline__ void put(float* s, int r, int c, const uint4& v) {
-    *reinterpret_cast<uint4*>(s + r * kLd + 4 * c) = v;
+  static __device__ __forceinline__ void put(float* s, int r, int c, const u32x4& v) {
+    *reinterpret_cast<u32x4*>(s + r * kLd + 4 * c) = v;
   }
   static __device__ __forceinline__ f32x8 along(const float* s, int base, int ks, int lane) {
     const float* p = s + (base + (lane & 31)) * kLd + 16 * ks + 8 * (lane >> 5);
@@ -130,36 +131,114 @@ __device__ __forceinline__ f32x8 across(const float* s, int base, int dt, int la
   return out;
 }
 
-// A tile of ROWS rows x DP elements on its way from memory to LDS through the
-// registers of THREADS threads; rows past `rows` and elements past d are zero,
-// whatever memory holds there.
-template <typename T, int DP, int ROWS, int THREADS> struct Stage {
-  static constexpr int kP = Tile<T, DP>::kPieces, kPer = ROWS * kP / THREADS;
-  static_assert(kPer * THREADS == ROWS * kP, "whole pieces per thread");
-  uint4 v[kPer];
-  // addr(row) gives the row's first element
-  template <typename Addr>
-  __device__ __forceinline__ void load(int tid, int rows, int d, Addr addr) {
-    constexpr int kE = 16 / sizeof(T);
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int x = tid + i * THREADS, r = x / kP, c = x % kP;
-      v[i] = make_uint4(0, 0, 0, 0);
-      if (r < rows && c * kE < d) v[i] = *reinterpret_cast<const uint4*>(addr(r) + c * kE);
-    }
-  }
-  __device__ __forceinline__ void store(int tid, T* s) const {
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int x = tid + i * THREADS;
-      Tile<T, DP>::put(s, x / kP, x % kP, v[i]);
-    }
-  }
-};
-
 // x / group for 0 <= x < 2^20: the quotient of x + 1/2 stays at least 1 / (2 group)
 // away from a whole number, far more than the product's rounding.
 __device__ __forceinline__ int div_group(int x, float inv_group) { return (int)(((float)x + 0.5f) * inv_group); }
+
+// Buffer resource over `bytes` bytes from a uniform address: loads outside give
+// zero (raw buffer, 32-bit data).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* base, int64_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00027000);
+}
+constexpr uint32_t kOutside = 0x80000000u;         // an offset past every such buffer
+
+// Row strides up to which a tile of at most 129 rows lies within 2^31 bytes.
+inline bool narrow_stride(int64_t ld, int size) { return ld * size <= (int64_t)1 << 23; }
+
+// A tile of ROWS rows x DP elements on its way from memory to LDS through the
+// registers of THREADS threads.  Rows past the end and elements past d are zero,
+// whatever memory holds there: buffer loads return zero outside their range,
+// which costs no instruction, where row strides allow 32-bit offsets (narrow),
+// and the others select.
+template <typename T, int DP, int ROWS, int THREADS> struct Stage {
+  static constexpr int kP = Tile<T, DP>::kPieces, kPer = ROWS * kP / THREADS, kE = 16 / sizeof(T), kStep = THREADS / kP;
+  static_assert(kPer * THREADS == ROWS * kP && kStep * kP == THREADS, "whole pieces per thread");
+  u32x4 v[kPer];
+  // rows >= 1 rows from `base` (uniform), ld apart
+  __device__ __forceinline__ void load(int tid, const T* base, int64_t ld, int rows, int d, bool narrow) {
+    const int r0 = tid / kP, c = tid % kP;
+    if (narrow) {
+      const auto rs = buffer(base, ((int64_t)(rows - 1) * ld + d) * (int)sizeof(T));
+      const uint32_t ldb = (uint32_t)ld * sizeof(T), at = c * kE < d ? r0 * ldb + c * 16 : kOutside;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, at + i * (kStep * ldb), 0, 0));
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int r = r0 + i * kStep;
+        v[i] = u32x4{0, 0, 0, 0};
+        if (r < rows && c * kE < d) v[i] = *reinterpret_cast<const u32x4*>(base + r * ld + c * kE);
+      }
+    }
+  }
+  // rows x = g0 .. of `queries` tokens from `base` (uniform; first token, first head
+  // of the group): row x is token x / group, head x % group
+  __device__ __forceinline__ void load_group(int tid, const T* base, int64_t ld, int queries, int g0, int group,
+                                             float inv_group, int d, bool narrow) {
+    const int r0 = tid / kP, c = tid % kP;
+    if (narrow) {
+      const auto rs = buffer(base, ((int64_t)(queries - 1) * ld + (int64_t)group * d) * (int)sizeof(T));
+      const uint32_t ldb = (uint32_t)ld * sizeof(T), db = (uint32_t)d * sizeof(T);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int x = g0 + r0 + i * kStep, tg = div_group(x, inv_group);
+        const uint32_t at = c * kE < d ? tg * ldb + (x - tg * group) * db + c * 16 : kOutside;
+        v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, at, 0, 0));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int x = g0 + r0 + i * kStep, tg = div_group(x, inv_group);
+        v[i] = u32x4{0, 0, 0, 0};
+        if (tg < queries && c * kE < d)
+          v[i] = *reinterpret_cast<const u32x4*>(base + tg * ld + (int64_t)(x - tg * group) * d + c * kE);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(int tid, T* s) const {
+    const int r0 = tid / kP, c = tid % kP;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) Tile<T, DP>::put(s, r0 + i * kStep, c, v[i]);
+  }
+};
+
+// Nothing is moved across by the compiler.  The product loops read the fragments
+// of a step before the products of the step before it; left alone the compiler
+// sinks each read to its product, which then waits for LDS.
+__device__ __forceinline__ void pin() { __builtin_amdgcn_sched_barrier(0); }
+
+// by: 1, -1 or 0 (exact)
+template <typename T, typename F, int N>
+__device__ __forceinline__ void multiply(F (&x)[N], float by) {
+  if (by != 1.f)
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[k][u] = (T)((float)x[k][u] * by);
+}
+
+template <int DP, typename T, typename F>
+__device__ __forceinline__ void read_along(const T* s, int base, int lane, F (&out)[DP / 16]) {
+#pragma unroll
+  for (int ks = 0; ks < DP / 16; ++ks) out[ks] = Tile<T, DP>::along(s, base, ks, lane);
+}
+template <int DP, typename T, typename F>
+__device__ __forceinline__ void read_across(const T* s, int base, int lane, const uint32_t (&tr)[2], F (&out)[DP / 32]) {
+#pragma unroll
+  for (int dt = 0; dt < DP / 32; ++dt) out[dt] = across<DP>(s, base, dt, lane, tr);
+}
+template <int N, typename F>
+__device__ __forceinline__ f32x16 product(const F (&a)[N], const F (&b)[N], f32x16 s = f32x16{}) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) s = mma32(a[k], b[k], s);
+  return s;
+}
+template <int N, typename F>
+__device__ __forceinline__ void add_products(const F (&a)[N], const F& b, f32x16 (&acc)[N]) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) acc[k] = mma32(a[k], b, acc[k]);
+}
 
 // Sum over the two lanes l, l ^ 32 that hold one column of an accumulator.
 __device__ __forceinline__ float pair_sum(float v) {
