@@ -8,6 +8,7 @@ back to any other implementation.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 
 import numpy as np
@@ -146,7 +147,7 @@ def load(path: str = LIB_PATH):
 
 
 def _check(status: int):
-    if status != NT_OK:
+    if status:
         raise NtError(status, load().nt_last_error().decode())
 
 
@@ -648,20 +649,33 @@ def nt_pair_row_attention_backward(layout: NestedLayout, axis: int, heads: int, 
 
 
 # ---------------------------------------------------------------- tokens
-def _same_device(*named):
-    """Raises unless every tensor given is on the current device."""
-    dev = _t().cuda.current_device()
-    for name, t in named:
-        if t is not None and (not t.is_cuda or t.device.index != dev):
-            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{dev}")
+def _device() -> int:
+    return _t()._C._cuda_getDevice()
 
 
-def _rows(t, name, rows, cols):
-    """(device pointer, row stride) of a [rows, cols] operand."""
-    p, ld = _mat(t, name)
-    if t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"{name} must be [{rows}, {cols}], got {list(t.shape)}")
-    return p, ld
+def _rows(t, name, rows, cols, dev, dtype=None):
+    """(device pointer, row stride) of a [rows, cols] operand on device `dev`."""
+    shape = t.shape
+    if len(shape) != 2 or shape[0] != rows or shape[1] != cols:
+        raise ValueError(f"{name} must be [{rows}, {cols}], got {list(shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{dev}")
+    if rows <= 1 or cols == 0:
+        if rows == 1 and cols > 1 and t.stride(1) != 1:
+            raise ValueError(f"{name} must have contiguous rows")
+        return t.data_ptr(), cols
+    ld, unit = t.stride()
+    if unit != 1 and cols > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return t.data_ptr(), ld
+
+
+def _workspace_on(ws, dev):
+    if ws is not None and ws.get_device() != dev:
+        raise ValueError(f"workspace is on {ws.device}, the current device is cuda:{dev}")
+    return _ws(ws)
 
 
 def _window_args(q_layout, heads, head_dim, kv_layout, kv_heads, left, right, sinks, scale, dtype) -> WindowArgs:
@@ -672,7 +686,7 @@ def _window_args(q_layout, heads, head_dim, kv_layout, kv_heads, left, right, si
     a.heads, a.head_dim = int(heads), int(head_dim)
     a.kv_heads = a.heads if kv_heads is None else int(kv_heads)
     a.left, a.right, a.sinks = int(left), int(right), int(sinks)
-    a.scale = 1.0 / float(np.sqrt(head_dim)) if scale is None else float(scale)
+    a.scale = 1.0 / math.sqrt(head_dim) if scale is None else float(scale)
     a.dtype = dtype
     return a
 
@@ -698,20 +712,16 @@ def window_attention_backward_workspace_bytes(q_layout: NestedLayout, heads: int
     return int(n.value)
 
 
-def _window_operands(a, q_layout, kv_layout, q, k, v, o, lse):
+def _window_operands(a, q_layout, kv_layout, q, k, v, o, lse, dev):
     nq, nk = q_layout.sum_n, (q_layout if kv_layout is None else kv_layout).sum_n
     cq, ck = a.heads * a.head_dim, a.kv_heads * a.head_dim
-    if not (q.dtype == k.dtype == v.dtype == o.dtype):
-        raise ValueError("q, k, v and o must share one dtype")
-    a.q, a.ld_q = _rows(q, "q", nq, cq)
-    a.k, a.ld_k = _rows(k, "k", nk, ck)
-    a.v, a.ld_v = _rows(v, "v", nk, ck)
-    a.o, a.ld_o = _rows(o, "o", nq, cq)
+    dt = q.dtype
+    a.q, a.ld_q = _rows(q, "q", nq, cq, dev)
+    a.k, a.ld_k = _rows(k, "k", nk, ck, dev, dt)
+    a.v, a.ld_v = _rows(v, "v", nk, ck, dev, dt)
+    a.o, a.ld_o = _rows(o, "o", nq, cq, dev, dt)
     if lse is not None:
-        if lse.dtype != _t().float32:
-            raise ValueError("lse must be float32")
-        a.lse, a.ld_lse = _rows(lse, "lse", a.heads, nq)
-        a.ld_lse = max(a.ld_lse, nq)
+        a.lse, a.ld_lse = _rows(lse, "lse", a.heads, nq, dev, _torch.float32)
     return nq, nk, cq, ck
 
 
@@ -726,20 +736,20 @@ def nt_window_attention(q_layout: NestedLayout, heads: int, head_dim: int, q, k,
     [heads, sum N] (needed by the backward) or None; kv_lengths: device int32
     [batch], the keys in use of each sample's slots, or None."""
     a = _window_args(q_layout, heads, head_dim, kv_layout, kv_heads, left, right, sinks, scale, _dtype(q))
-    _same_device(("q", q), ("k", k), ("v", v), ("o", o), ("lse", lse), ("kv_lengths", kv_lengths),
-                 ("workspace", workspace))
-    _window_operands(a, q_layout, kv_layout, q, k, v, o, lse)
+    dev = _device()
+    _window_operands(a, q_layout, kv_layout, q, k, v, o, lse, dev)
     if kv_lengths is not None:
-        if kv_lengths.dtype != _t().int32 or kv_lengths.dim() != 1 or kv_lengths.shape[0] != q_layout.batch \
-                or not kv_lengths.is_contiguous():
-            raise ValueError("kv_lengths must be contiguous int32 [batch]")
+        if kv_lengths.dtype != _torch.int32 or kv_lengths.shape != (q_layout.batch,) or not kv_lengths.is_contiguous() \
+                or kv_lengths.get_device() != dev:
+            raise ValueError("kv_lengths must be contiguous int32 [batch] on the current device")
         a.kv_lengths = kv_lengths.data_ptr()
     if workspace is None:
         n = C.c_uint64()
         _check(load().nt_window_attention_workspace(C.byref(a), C.byref(n)))
         workspace = workspace_tensor(int(n.value))
-    a.workspace, a.workspace_bytes = _ws(workspace)
-    _check(load().nt_window_attention(C.byref(a), _stream()))
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = _workspace_on(workspace, dev)
+    _check(_lib.nt_window_attention(C.byref(a), _stream()))
     return o
 
 
@@ -749,40 +759,39 @@ def nt_window_attention_backward(q_layout: NestedLayout, heads: int, head_dim: i
     """Gradients of nt_window_attention from its operands, its output o and lse,
     and the output's gradient; dq, dk, dv are overwritten."""
     a = _window_args(q_layout, heads, head_dim, kv_layout, kv_heads, left, right, sinks, scale, _dtype(q))
-    _same_device(("q", q), ("k", k), ("v", v), ("o", o), ("lse", lse), ("dout", dout), ("dq", dq), ("dk", dk),
-                 ("dv", dv), ("workspace", workspace))
-    nq, nk, cq, ck = _window_operands(a, q_layout, kv_layout, q, k, v, o, lse)
-    if any(t.dtype != q.dtype for t in (dout, dq, dk, dv)):
-        raise ValueError("dout, dq, dk and dv must have the dtype of q")
-    a.dout, a.ld_dout = _rows(dout, "dout", nq, cq)
-    a.dq, a.ld_dq = _rows(dq, "dq", nq, cq)
-    a.dk, a.ld_dk = _rows(dk, "dk", nk, ck)
-    a.dv, a.ld_dv = _rows(dv, "dv", nk, ck)
+    dev, dt = _device(), q.dtype
+    nq, nk, cq, ck = _window_operands(a, q_layout, kv_layout, q, k, v, o, lse, dev)
+    a.dout, a.ld_dout = _rows(dout, "dout", nq, cq, dev, dt)
+    a.dq, a.ld_dq = _rows(dq, "dq", nq, cq, dev, dt)
+    a.dk, a.ld_dk = _rows(dk, "dk", nk, ck, dev, dt)
+    a.dv, a.ld_dv = _rows(dv, "dv", nk, ck, dev, dt)
     if workspace is None:
         n = C.c_uint64()
         _check(load().nt_window_attention_backward_workspace(C.byref(a), C.byref(n)))
         workspace = workspace_tensor(int(n.value))
-    a.workspace, a.workspace_bytes = _ws(workspace)
-    _check(load().nt_window_attention_backward(C.byref(a), _stream()))
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = _workspace_on(workspace, dev)
+    _check(_lib.nt_window_attention_backward(C.byref(a), _stream()))
     return dq, dk, dv
 
 
-def _ids(ids):
-    torch = _t()
-    if ids.dim() != 1 or not ids.is_contiguous() or ids.dtype not in (torch.int32, torch.int64):
+def _ids(ids, dev):
+    dt, shape = ids.dtype, ids.shape
+    if len(shape) != 1 or (dt != _torch.int64 and dt != _torch.int32) or not ids.is_contiguous():
         raise ValueError("ids must be contiguous 1-D int32 or int64")
-    return ids.data_ptr(), int(ids.dtype == torch.int64), ids.shape[0]
+    if ids.get_device() != dev:
+        raise ValueError(f"ids is on {ids.device}, the current device is cuda:{dev}")
+    return ids.data_ptr(), dt == _torch.int64, shape[0]
 
 
 def nt_embedding(table, ids, y, scale: float = 1.0):
     """y[r] = scale * table[ids[r]]; an id outside the table gives a row of zeros."""
-    _same_device(("table", table), ("ids", ids), ("y", y))
-    pi, wide, rows = _ids(ids)
+    dev = _device()
+    pi, wide, rows = _ids(ids, dev)
     vocab, c = table.shape
-    pt, ldt = _mat(table, "table")
-    py, ldy = _rows(y, "y", rows, c)
-    _check(load().nt_embedding(pt, vocab, ldt, _dtype(table), pi, wide, rows, c, float(scale), py, ldy, _dtype(y),
-                               _stream()))
+    pt, ldt = _rows(table, "table", vocab, c, dev)
+    py, ldy = _rows(y, "y", rows, c, dev)
+    _check(load().nt_embedding(pt, vocab, ldt, _dtype(table), pi, wide, rows, c, scale, py, ldy, _dtype(y), _stream()))
     return y
 
 
@@ -794,16 +803,16 @@ def embedding_backward_workspace_bytes(rows: int, vocab: int, c: int) -> int:
 
 def nt_embedding_backward(ids, dy, dtable, scale: float = 1.0, accumulate: bool = False, workspace=None):
     """dtable[v] (+)= scale * sum of dy over the rows with id v (fp32 or bf16 dtable)."""
-    _same_device(("ids", ids), ("dy", dy), ("dtable", dtable), ("workspace", workspace))
-    pi, wide, rows = _ids(ids)
+    dev = _device()
+    pi, wide, rows = _ids(ids, dev)
     vocab, c = dtable.shape
-    py, ldy = _rows(dy, "dy", rows, c)
-    pt, ldt = _mat(dtable, "dtable")
+    py, ldy = _rows(dy, "dy", rows, c, dev)
+    pt, ldt = _rows(dtable, "dtable", vocab, c, dev)
     if workspace is None:
         workspace = workspace_tensor(embedding_backward_workspace_bytes(rows, vocab, c))
-    pw, nw = _ws(workspace)
-    _check(load().nt_embedding_backward(pi, wide, rows, vocab, c, py, ldy, _dtype(dy), float(scale), pt, ldt,
-                                        _dtype(dtable), int(bool(accumulate)), pw, nw, _stream()))
+    pw, nw = _workspace_on(workspace, dev)
+    _check(load().nt_embedding_backward(pi, wide, rows, vocab, c, py, ldy, _dtype(dy), scale, pt, ldt, _dtype(dtable),
+                                        bool(accumulate), pw, nw, _stream()))
     return dtable
 
 

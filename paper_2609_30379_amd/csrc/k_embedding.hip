@@ -7,6 +7,8 @@
 // one id inside a chunk goes straight to its table row, a run that crosses chunks
 // leaves one partial sum per chunk, which a last launch adds in order.  There are
 // no floating-point atomics: the result does not depend on timing.
+#include <algorithm>
+
 #include "nt_device.h"
 #include "nt_internal.h"
 
@@ -89,11 +91,14 @@ embedding_kernel(const TT* __restrict__ table, int64_t ld_table, uint32_t vocab,
 }
 
 // ---------------------------------------------------------------- sort by id
-// Least-significant-digit radix sort of (id, row) pairs, kTile pairs per
-// workgroup.  A pass counts the digits of every tile, then every tile finds
-// where its pairs of each digit begin (all smaller digits, and the same digit in
-// the tiles before) and writes them there in their order.
-constexpr int kTile = 4096, kMaxBins = 512;
+// Stable least-significant-digit radix sort of (id, row) pairs.  Up to kSmall
+// pairs are sorted by one workgroup in LDS, all passes in one launch.  More go
+// through two launches per pass: one counts the digits of every tile, the other
+// finds where a tile's pairs of each digit begin (all smaller digits, and the
+// same digit in the tiles before) and writes them there in their order.  The
+// gradient table is cleared meanwhile by further workgroups of the same launches:
+// the sort is short and latency-bound, the clearing long and bound by bytes.
+constexpr int kSmall = 4096, kSmallBits = 8, kMaxBins = 512;
 
 struct SortParams {
   const void* ids;               // first pass: the tokens; later passes: NULL
@@ -103,117 +108,222 @@ struct SortParams {
   uint32_t *key_out, *row_out;
   uint32_t* hist;                // [tiles][bins]
   int64_t rows;
-  int tiles, shift, bits;
-  char* fill;                    // a share of the gradient's memory to clear: rows fill_lo .. fill_hi
-  int64_t fill_ld, fill_lo, fill_hi;   // bytes per row, first row, end
-  int fill_bytes;                // bytes of a row that are cleared
+  int tiles, shift, bits, passes;
+  char* fill;                    // pieces fill_lo .. fill_hi of the gradient's memory are cleared, each fill_bytes long
+  int64_t fill_ld, fill_lo, fill_hi, fill_total;   // and fill_ld apart; nothing past fill_total bytes
+  int fill_bytes;
 };
 
 __device__ __forceinline__ uint32_t sort_key(const SortParams& p, int64_t r) {
   return p.ids ? token(p.ids, p.wide, r, p.vocab) : p.key_in[r];
 }
 
-// Workgroups past the tiles clear the gradient table's rows: one wave per row
-// and turn, 16 bytes per lane.
-__device__ __forceinline__ void clear_rows(const SortParams& p, int64_t wave, int64_t waves, int lane) {
+// One wave per piece and turn, 16 bytes per lane and store.
+__device__ __forceinline__ void clear_pieces(const SortParams& p, int64_t wave, int64_t waves, int lane) {
   for (int64_t r = p.fill_lo + wave; r < p.fill_hi; r += waves) {
-    char* d = p.fill + r * p.fill_ld;
-    for (int b = lane * 16; b < p.fill_bytes; b += 1024) *reinterpret_cast<uint4*>(d + b) = make_uint4(0, 0, 0, 0);
+    const int64_t at = r * p.fill_ld;
+    const int n = (int)min((int64_t)p.fill_bytes, p.fill_total - at);
+    for (int b = lane * 16; b < n; b += 1024) *reinterpret_cast<uint4*>(p.fill + at + b) = make_uint4(0, 0, 0, 0);
   }
 }
 
+// Lanes that hold the same digit as this one, among those in `ok`: one ballot per bit.
+__device__ __forceinline__ uint64_t same_digit(uint32_t dg, int bits, uint64_t ok) {
+  for (int bit = 0; bit < bits; ++bit) {
+    const uint64_t set = __ballot((dg >> bit) & 1);
+    ok &= (dg >> bit) & 1 ? set : ~set;
+  }
+  return ok;
+}
+__device__ __forceinline__ uint32_t lanes_below(uint64_t m) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+}
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v, int lane) {      // inclusive
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const uint32_t u = __shfl_up(v, s, 64);
+    v += lane >= s ? u : 0;
+  }
+  return v;
+}
+
+__global__ void __launch_bounds__(1024)
+sort_small_kernel(SortParams p) {
+  constexpr int kIter = kSmall / 1024, kBins = 1 << kSmallBits;
+  __shared__ uint32_t keys[kSmall], rows[kSmall], wc[16][kBins], sums[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (blockIdx.x > 0) {
+    clear_pieces(p, ((int64_t)blockIdx.x - 1) * 16 + wave, ((int64_t)gridDim.x - 1) * 16, lane);
+    return;
+  }
+  const int n = (int)p.rows, bins = 1 << p.bits;
+#pragma unroll
+  for (int k = 0; k < kIter; ++k) {
+    const int r = tid + 1024 * k;
+    if (r < n) {
+      keys[r] = token(p.ids, p.wide, r, p.vocab);
+      rows[r] = r;
+    }
+  }
+  for (int pass = 0; pass < p.passes; ++pass) {
+    const int shift = pass * p.bits;
+    for (int b = tid; b < 16 * kBins; b += 1024) (&wc[0][0])[b] = 0;
+    __syncthreads();
+    uint32_t key[kIter], row[kIter], rank[kIter];
+#pragma unroll
+    for (int k = 0; k < kIter; ++k) {                      // wave w ranks a sixteenth of the pairs in order
+      const int r = wave * (kSmall / 16) + k * 64 + lane;
+      const bool ok = r < n;
+      key[k] = ok ? keys[r] : 0;
+      row[k] = ok ? rows[r] : 0;
+      const uint32_t dg = (key[k] >> shift) & (bins - 1);
+      const uint64_t same = same_digit(dg, p.bits, __ballot(ok));
+      const uint32_t old = wc[wave][dg], below = lanes_below(same);
+      rank[k] = old + below;
+      if (ok && below == 0) wc[wave][dg] = old + __popcll(same);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    uint32_t tot = 0, incl = 0;
+    if (tid < kBins) {                                     // counts become the places before each wave's first pair
+#pragma unroll
+      for (int w = 0; w < 16; ++w) {
+        const uint32_t c = wc[w][tid];
+        wc[w][tid] = tot;
+        tot += c;
+      }
+      incl = wave_scan(tot, lane);
+      if (lane == 63) sums[wave] = incl;
+    }
+    __syncthreads();
+    if (tid < kBins) {
+      uint32_t base = incl - tot;
+      for (int w = 0; w < wave; ++w) base += sums[w];
+#pragma unroll
+      for (int w = 0; w < 16; ++w) wc[w][tid] += base;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kIter; ++k) {
+      const int r = wave * (kSmall / 16) + k * 64 + lane;
+      if (r < n) {
+        const uint32_t to = wc[wave][(key[k] >> shift) & (bins - 1)] + rank[k];
+        keys[to] = key[k];
+        rows[to] = row[k];
+      }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int k = 0; k < kIter; ++k) {
+    const int r = tid + 1024 * k;
+    if (r < n) {
+      p.key_out[r] = keys[r];
+      p.row_out[r] = rows[r];
+    }
+  }
+}
+
+template <int ITER>
 __global__ void __launch_bounds__(256)
 sort_count_kernel(SortParams p) {
   __shared__ uint32_t h[kMaxBins];
   const int tid = threadIdx.x;
   if ((int)blockIdx.x >= p.tiles) {
     const int64_t w = ((int64_t)blockIdx.x - p.tiles) * 4 + (tid >> 6);
-    clear_rows(p, w, ((int64_t)gridDim.x - p.tiles) * 4, tid & 63);
+    clear_pieces(p, w, ((int64_t)gridDim.x - p.tiles) * 4, tid & 63);
     return;
   }
   const int bins = 1 << p.bits;
+  uint32_t key[ITER];
+  const int64_t r0 = (int64_t)blockIdx.x * (ITER * 256);
+#pragma unroll
+  for (int k = 0; k < ITER; ++k) {
+    const int64_t r = r0 + k * 256 + tid;
+    key[k] = r < p.rows ? sort_key(p, r) : 0;
+  }
   for (int b = tid; b < bins; b += 256) h[b] = 0;
   __syncthreads();
-  const int64_t r0 = (int64_t)blockIdx.x * kTile;
 #pragma unroll
-  for (int k = 0; k < kTile / 256; ++k) {
-    const int64_t r = r0 + k * 256 + tid;
-    if (r < p.rows) atomicAdd(&h[(sort_key(p, r) >> p.shift) & (bins - 1)], 1u);
-  }
+  for (int k = 0; k < ITER; ++k)
+    if (r0 + k * 256 + tid < p.rows) atomicAdd(&h[(key[k] >> p.shift) & (bins - 1)], 1u);
   __syncthreads();
   for (int b = tid; b < bins; b += 256) p.hist[(int64_t)blockIdx.x * bins + b] = h[b];
 }
 
+template <int ITER>
 __global__ void __launch_bounds__(256)
 sort_scatter_kernel(SortParams p) {
-  __shared__ uint32_t base[kMaxBins], wc[4][kMaxBins], part[256];
+  __shared__ uint32_t wc[4][kMaxBins], sums[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if ((int)blockIdx.x >= p.tiles) {
     const int64_t w = ((int64_t)blockIdx.x - p.tiles) * 4 + wave;
-    clear_rows(p, w, ((int64_t)gridDim.x - p.tiles) * 4, lane);
+    clear_pieces(p, w, ((int64_t)gridDim.x - p.tiles) * 4, lane);
     return;
   }
-  const int bins = 1 << p.bits, per = (bins + 255) / 256, tile = blockIdx.x;
-  // thread b takes bins b per .. b per + per - 1: totals, and the tiles before
-  uint32_t tot[2] = {0, 0}, before[2] = {0, 0};
-  for (int u = 0; u < per; ++u) {
-    const int b = tid * per + u;
-    if (b < bins)
-      for (int t = 0; t < p.tiles; ++t) {
-        const uint32_t c = p.hist[(int64_t)t * bins + b];
-        tot[u] += c;
-        before[u] += t < tile ? c : 0;
-      }
-  }
-  part[tid] = tot[0] + tot[1];
-  for (int b = tid; b < 4 * kMaxBins; b += 256) (&wc[0][0])[b] = 0;
-  __syncthreads();
-  for (int s = 1; s < 256; s <<= 1) {                    // inclusive scan of the threads' totals
-    const uint32_t v = tid >= s ? part[tid - s] : 0;
-    __syncthreads();
-    part[tid] += v;
-    __syncthreads();
-  }
-  uint32_t at = part[tid] - tot[0] - tot[1];
-  for (int u = 0; u < per; ++u) {
-    const int b = tid * per + u;
-    if (b < bins) base[b] = at + before[u];
-    at += tot[u];
-  }
-  // ranks: wave w takes a quarter of the tile in order, 64 pairs at a time; the
-  // lanes that hold equal digits are found by one ballot per digit bit
-  constexpr int kIter = kTile / 256;
-  uint32_t key[kIter], rank[kIter];
-  const int64_t r0 = (int64_t)tile * kTile + wave * (kTile / 4);
+  const int bins = 1 << p.bits, tile = blockIdx.x;
+  // wave w takes a quarter of the tile in order, 64 pairs at a time
+  uint32_t key[ITER], row[ITER], rank[ITER];
+  const int64_t r0 = (int64_t)tile * (ITER * 256) + wave * (ITER * 64);
 #pragma unroll
-  for (int k = 0; k < kIter; ++k) {
+  for (int k = 0; k < ITER; ++k) {
     const int64_t r = r0 + k * 64 + lane;
-    const bool ok = r < p.rows;
-    key[k] = ok ? sort_key(p, r) : 0;
-    const uint32_t dg = (key[k] >> p.shift) & (bins - 1);
-    uint64_t same = __ballot(ok);
-    for (int bit = 0; bit < p.bits; ++bit) {
-      const uint64_t set = __ballot((dg >> bit) & 1);
-      same &= (dg >> bit) & 1 ? set : ~set;
+    key[k] = r < p.rows ? sort_key(p, r) : 0;
+    row[k] = r < p.rows ? (p.ids ? (uint32_t)r : p.row_in[r]) : 0;
+  }
+  for (int b = tid; b < 4 * kMaxBins; b += 256) (&wc[0][0])[b] = 0;
+  // thread t has the digits 2 t and 2 t + 1: their totals, and the tiles before
+  uint32_t t0 = 0, t1 = 0, b0 = 0, b1 = 0;
+  if (2 * tid < bins)
+#pragma unroll 8
+    for (int t = 0; t < p.tiles; ++t) {
+      const uint2 c = *reinterpret_cast<const uint2*>(p.hist + (int64_t)t * bins + 2 * tid);
+      t0 += c.x;
+      t1 += c.y;
+      b0 += t < tile ? c.x : 0;
+      b1 += t < tile ? c.y : 0;
     }
-    const uint32_t old = wc[wave][dg], below = __popcll(same & ((1ull << lane) - 1));
+  const uint32_t incl = wave_scan(t0 + t1, lane);
+  if (lane == 63) sums[wave] = incl;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < ITER; ++k) {
+    const bool ok = r0 + k * 64 + lane < p.rows;
+    const uint32_t dg = (key[k] >> p.shift) & (bins - 1);
+    const uint64_t same = same_digit(dg, p.bits, __ballot(ok));
+    const uint32_t old = wc[wave][dg], below = lanes_below(same);
     rank[k] = old + below;
     if (ok && below == 0) wc[wave][dg] = old + __popcll(same);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  __syncthreads();
+  if (2 * tid < bins) {
+    uint32_t at = incl - t0 - t1;
+    for (int w = 0; w < wave; ++w) at += sums[w];
+    uint32_t x = at + b0, y = at + t0 + b1;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {                          // counts become the places before each wave's first pair
+      const uint32_t c = wc[w][2 * tid], d = wc[w][2 * tid + 1];
+      wc[w][2 * tid] = x;
+      wc[w][2 * tid + 1] = y;
+      x += c;
+      y += d;
+    }
   }
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < kIter; ++k) {
-    const int64_t r = r0 + k * 64 + lane;
-    if (r >= p.rows) continue;
-    const uint32_t dg = (key[k] >> p.shift) & (bins - 1);
-    uint32_t to = base[dg] + rank[k];
-    for (int w = 0; w < wave; ++w) to += wc[w][dg];
+  for (int k = 0; k < ITER; ++k) {
+    if (r0 + k * 64 + lane >= p.rows) continue;
+    const uint32_t to = wc[wave][(key[k] >> p.shift) & (bins - 1)] + rank[k];
     p.key_out[to] = key[k];
-    p.row_out[to] = p.ids ? (uint32_t)r : p.row_in[r];
+    p.row_out[to] = row[k];
   }
 }
 
 // ---------------------------------------------------------------- sum of runs
+constexpr int kBatch = 8;          // rows in flight per thread
 struct SumParams {
   const uint32_t *key, *row;
   uint32_t vocab;
@@ -257,27 +367,36 @@ embedding_sum_kernel(SumParams p, const TD* __restrict__ dy, int64_t ld_dy, TG* 
   float acc[8] = {};
   uint32_t cur = p.key[s];
   bool enters = s > 0 && p.key[s - 1] == cur;
-  for (int64_t x = s; x < e; ++x) {
-    const uint32_t k = p.key[x];
-    if (k != cur) {
-      if (cur < p.vocab) {
-        if (enters) {
+  for (int64_t x0 = s; x0 < e && cur < p.vocab; x0 += kBatch) {
+    // the batch's rows in flight together; then in order
+    uint32_t id[kBatch];
+    Row8<TD> v[kBatch];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) p.part[((ch * 2) * p.cv + piece) * kVE + j] = acc[j];
+    for (int u = 0; u < kBatch; ++u) {
+      const int64_t x = min(x0 + u, e - 1);
+      id[u] = p.key[x];
+      v[u].load(dy + (int64_t)p.row[x] * ld_dy + c);
+    }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      if (x0 + u >= e || cur >= p.vocab) break;
+      if (id[u] != cur) {
+        if (enters) {
+          float* d = p.part + (ch * 2 * p.cv + piece) * kVE;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) d[j] = acc[j];
         } else {
           write_row(dtable, ld, cur, c, acc, p);
         }
+        cur = id[u];
+        enters = false;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+        if (cur >= p.vocab) break;                         // sorted: only tokens outside the table follow
       }
-      cur = k;
-      enters = false;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+      for (int j = 0; j < 8; ++j) acc[j] += v[u].v[j];
     }
-    if (k >= p.vocab) break;                             // sorted: only tokens outside the table follow
-    Row8<TD> v;
-    v.load(dy + (int64_t)p.row[x] * ld_dy + c);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] += v.v[j];
   }
   if (cur >= p.vocab) return;
   const bool leaves = e < p.rows && p.key[e] == cur;
@@ -308,18 +427,40 @@ embedding_join_kernel(SumParams p, TG* __restrict__ dtable, int64_t ld) {
   const float* d = p.part + ((ch * 2 + 1) * p.cv + piece) * kVE;
 #pragma unroll
   for (int j = 0; j < 8; ++j) acc[j] = d[j];
-  for (int64_t x = ch + 1; x < p.chunks && p.key[x * p.chunk] == id; ++x) {
-    const float* h = p.part + ((x * 2) * p.cv + piece) * kVE;
+  const float* h = p.part + piece * kVE;                   // chunk x's part of the run that enters: h + 2 x 8 cv
+  bool more = true;
+  for (int64_t x = ch + 1; more; x += kBatch) {
+    bool in[kBatch];
+    Row8<float> v[kBatch];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] += h[j];
+    for (int u = 0; u < kBatch; ++u) {
+      const int64_t y = min(x + u, p.chunks - 1);
+      in[u] = x + u < p.chunks && p.key[y * p.chunk] == id;   // sorted: once false, false from there on
+      v[u].load(h + y * 2 * p.cv * kVE);
+    }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      if (!in[u]) {
+        more = false;
+        break;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] += v[u].v[j];
+    }
   }
   write_row(dtable, ld, id, piece * kVE, acc, p);
 }
 
-constexpr int kChunk = 32;
+// Sorted rows per chunk: 32, and up to 128 where there are 2048 chunks or more all
+// the same; longer chunks leave fewer partial sums to add.
+int chunk_of(int64_t rows) { return rows < 1 << 17 ? 32 : rows < 1 << 18 ? 64 : 128; }
+// Pairs per tile / 256: small tiles where few would leave the sort to a handful of
+// workgroups, large ones where every tile adds up the counts of many.
+int tile_iter(int64_t rows) { return rows <= 1 << 17 ? 4 : 16; }
 
 struct Plan {
-  int tiles, passes, bits;
+  bool small;
+  int tiles, passes, bits, chunk, iter;
   int64_t chunks;
   size_t key[2], row[2], hist, part, bytes;
 };
@@ -327,17 +468,21 @@ Plan plan(int64_t rows, int64_t vocab, int C) {
   Plan s{};
   int bits = 1;
   while ((vocab >> bits) > 0) ++bits;                    // ids 0 .. vocab
-  s.passes = (bits + 8) / 9;
+  s.small = rows <= kSmall;
+  const int most = s.small ? kSmallBits : 9;
+  s.passes = (bits + most - 1) / most;
   s.bits = (bits + s.passes - 1) / s.passes;
-  s.tiles = (int)((rows + kTile - 1) / kTile);
-  s.chunks = (rows + kChunk - 1) / kChunk;
+  s.iter = tile_iter(rows);
+  s.tiles = (int)((rows + s.iter * 256 - 1) / (s.iter * 256));
+  s.chunk = chunk_of(rows);
+  s.chunks = (rows + s.chunk - 1) / s.chunk;
   size_t at = 0;
   auto take = [&](size_t n) { const size_t o = at; at += (n + 15) / 16 * 16; return o; };
-  for (int k = 0; k < 2; ++k) {
+  for (int k = 0; k < (s.small ? 1 : 2); ++k) {
     s.key[k] = take((size_t)rows * 4);
     s.row[k] = take((size_t)rows * 4);
   }
-  s.hist = take((size_t)s.tiles * (1u << s.bits) * 4);
+  s.hist = take(s.small ? 0 : (size_t)s.tiles * (1u << s.bits) * 4);
   s.part = take((size_t)s.chunks * 2 * C * 4);
   s.bytes = at;
   return s;
@@ -353,35 +498,55 @@ hipError_t backward(const void* ids, int wide, int64_t rows, int64_t vocab, int 
   sp.rows = rows;
   sp.tiles = pl.tiles;
   sp.bits = pl.bits;
+  sp.passes = pl.passes;
   sp.hist = (uint32_t*)(ws + pl.hist);
+  // memory to clear: 4 KB pieces of a dense table, else its rows
   sp.fill = (char*)dtable;
-  sp.fill_ld = ld * (int64_t)sizeof(TG);
-  sp.fill_bytes = C * (int)sizeof(TG);
-  const int steps = 2 * pl.passes;                       // launches that share the clearing
-  for (int k = 0; k < steps; ++k) {
-    const int pass = k / 2;
-    sp.ids = pass ? nullptr : ids;
-    sp.key_in = (uint32_t*)(ws + pl.key[(pass + 1) & 1]);
-    sp.row_in = (uint32_t*)(ws + pl.row[(pass + 1) & 1]);
-    sp.key_out = (uint32_t*)(ws + pl.key[pass & 1]);
-    sp.row_out = (uint32_t*)(ws + pl.row[pass & 1]);
-    sp.shift = pass * pl.bits;
-    sp.fill_lo = accumulate ? 0 : vocab * k / steps;
-    sp.fill_hi = accumulate ? 0 : vocab * (k + 1) / steps;
-    const int64_t share = sp.fill_hi - sp.fill_lo;
-    const int clear = (int)(share <= 0 ? 0 : share < 8192 ? (share + 3) / 4 : 2048);
-    if (pl.tiles + clear == 0) continue;
-    if (k & 1) sort_scatter_kernel<<<pl.tiles + clear, 256, 0, s>>>(sp);
-    else sort_count_kernel<<<pl.tiles + clear, 256, 0, s>>>(sp);
+  const bool dense = ld == C;
+  sp.fill_bytes = dense ? 4096 : C * (int)sizeof(TG);
+  sp.fill_ld = dense ? 4096 : ld * (int64_t)sizeof(TG);
+  sp.fill_total = dense ? vocab * C * (int64_t)sizeof(TG) : INT64_MAX;
+  const int64_t pieces = accumulate ? 0 : dense ? (sp.fill_total + 4095) / 4096 : vocab;
+  int last = 0;                                          // which of the two pairs of arrays holds the result
+  if (pl.small) {
+    sp.ids = ids;
+    sp.key_out = (uint32_t*)(ws + pl.key[0]);
+    sp.row_out = (uint32_t*)(ws + pl.row[0]);
+    sp.fill_hi = pieces;
+    const int clear = (int)std::min<int64_t>((pieces + 15) / 16, 1024);
+    sort_small_kernel<<<1 + clear, 1024, 0, s>>>(sp);
     if (hipError_t e = hipGetLastError()) return e;
+  } else {
+    last = (pl.passes - 1) & 1;
+    const int steps = 2 * pl.passes;                     // launches that share the clearing
+    for (int k = 0; k < steps; ++k) {
+      const int pass = k / 2;
+      sp.ids = pass ? nullptr : ids;
+      sp.key_in = (uint32_t*)(ws + pl.key[(pass + 1) & 1]);
+      sp.row_in = (uint32_t*)(ws + pl.row[(pass + 1) & 1]);
+      sp.key_out = (uint32_t*)(ws + pl.key[pass & 1]);
+      sp.row_out = (uint32_t*)(ws + pl.row[pass & 1]);
+      sp.shift = pass * pl.bits;
+      sp.fill_lo = pieces * k / steps;
+      sp.fill_hi = pieces * (k + 1) / steps;
+      const int grid = pl.tiles + (int)std::min<int64_t>((sp.fill_hi - sp.fill_lo + 3) / 4, 2048);
+      if (k & 1) {
+        if (pl.iter == 4) sort_scatter_kernel<4><<<grid, 256, 0, s>>>(sp);
+        else sort_scatter_kernel<16><<<grid, 256, 0, s>>>(sp);
+      } else {
+        if (pl.iter == 4) sort_count_kernel<4><<<grid, 256, 0, s>>>(sp);
+        else sort_count_kernel<16><<<grid, 256, 0, s>>>(sp);
+      }
+      if (hipError_t e = hipGetLastError()) return e;
+    }
   }
   if (rows == 0) return hipSuccess;
   SumParams q{};
-  q.key = (uint32_t*)(ws + pl.key[(pl.passes - 1) & 1]);
-  q.row = (uint32_t*)(ws + pl.row[(pl.passes - 1) & 1]);
+  q.key = (uint32_t*)(ws + pl.key[last]);
+  q.row = (uint32_t*)(ws + pl.row[last]);
   q.vocab = (uint32_t)vocab;
   q.rows = rows;
-  q.chunk = kChunk;
+  q.chunk = pl.chunk;
   q.chunks = pl.chunks;
   q.cv = C / kVE;
   q.cvs = q.cv < 256 ? q.cv : 256;
