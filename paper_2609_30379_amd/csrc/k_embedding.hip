@@ -98,7 +98,7 @@ embedding_kernel(const TT* __restrict__ table, int64_t ld_table, uint32_t vocab,
 // same digit in the tiles before) and writes them there in their order.  The
 // gradient table is cleared meanwhile by further workgroups of the same launches:
 // the sort is short and latency-bound, the clearing long and bound by bytes.
-constexpr int kSmall = 4096, kSmallBits = 8, kMaxBins = 512;
+constexpr int kSmall = 16384, kSmallBits = 8, kMaxBins = 512;
 
 struct SortParams {
   const void* ids;               // first pass: the tokens; later passes: NULL
@@ -147,35 +147,41 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v, int lane) {      // in
   return v;
 }
 
+template <int ITER>
 __global__ void __launch_bounds__(1024)
 sort_small_kernel(SortParams p) {
-  constexpr int kIter = kSmall / 1024, kBins = 1 << kSmallBits;
-  __shared__ uint32_t keys[kSmall], rows[kSmall], wc[16][kBins], sums[4];
+  constexpr int kPairs = ITER * 1024, kBins = 1 << kSmallBits;
+  __shared__ uint32_t keys[kPairs], wc[16][kBins], sums[4];
+  __shared__ uint16_t rows[kPairs];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (blockIdx.x > 0) {
     clear_pieces(p, ((int64_t)blockIdx.x - 1) * 16 + wave, ((int64_t)gridDim.x - 1) * 16, lane);
     return;
   }
-  const int n = (int)p.rows, bins = 1 << p.bits;
+  const int n = (int)p.rows, bins = 1 << p.bits, r0 = wave * (ITER * 64) + lane;
+  // wave w has a sixteenth of the pairs in order, 64 at a time
+  uint32_t key[ITER], row[ITER], rank[ITER];
 #pragma unroll
-  for (int k = 0; k < kIter; ++k) {
-    const int r = tid + 1024 * k;
-    if (r < n) {
-      keys[r] = token(p.ids, p.wide, r, p.vocab);
-      rows[r] = r;
-    }
+  for (int k = 0; k < ITER; ++k) {
+    const int r = r0 + k * 64;
+    key[k] = r < n ? token(p.ids, p.wide, r, p.vocab) : 0;
+    row[k] = r;
   }
   for (int pass = 0; pass < p.passes; ++pass) {
     const int shift = pass * p.bits;
+    if (pass > 0) {
+#pragma unroll
+      for (int k = 0; k < ITER; ++k) {
+        const int r = r0 + k * 64;
+        key[k] = r < n ? keys[r] : 0;
+        row[k] = r < n ? rows[r] : 0;
+      }
+    }
     for (int b = tid; b < 16 * kBins; b += 1024) (&wc[0][0])[b] = 0;
     __syncthreads();
-    uint32_t key[kIter], row[kIter], rank[kIter];
 #pragma unroll
-    for (int k = 0; k < kIter; ++k) {                      // wave w ranks a sixteenth of the pairs in order
-      const int r = wave * (kSmall / 16) + k * 64 + lane;
-      const bool ok = r < n;
-      key[k] = ok ? keys[r] : 0;
-      row[k] = ok ? rows[r] : 0;
+    for (int k = 0; k < ITER; ++k) {
+      const bool ok = r0 + k * 64 < n;
       const uint32_t dg = (key[k] >> shift) & (bins - 1);
       const uint64_t same = same_digit(dg, p.bits, __ballot(ok));
       const uint32_t old = wc[wave][dg], below = lanes_below(same);
@@ -205,18 +211,16 @@ sort_small_kernel(SortParams p) {
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kIter; ++k) {
-      const int r = wave * (kSmall / 16) + k * 64 + lane;
-      if (r < n) {
-        const uint32_t to = wc[wave][(key[k] >> shift) & (bins - 1)] + rank[k];
-        keys[to] = key[k];
-        rows[to] = row[k];
-      }
+    for (int k = 0; k < ITER; ++k) {
+      if (r0 + k * 64 >= n) continue;
+      const uint32_t to = wc[wave][(key[k] >> shift) & (bins - 1)] + rank[k];
+      keys[to] = key[k];
+      rows[to] = (uint16_t)row[k];
     }
     __syncthreads();
   }
 #pragma unroll
-  for (int k = 0; k < kIter; ++k) {
+  for (int k = 0; k < ITER; ++k) {
     const int r = tid + 1024 * k;
     if (r < n) {
       p.key_out[r] = keys[r];
@@ -409,45 +413,60 @@ embedding_sum_kernel(SumParams p, const TD* __restrict__ dy, int64_t ld_dy, TG* 
   for (int j = 0; j < 8; ++j) d[j] = acc[j];
 }
 
-// The runs that cross chunks: the chunk in which one begins adds its parts.
+// The runs that cross chunks: the chunk in which one begins adds its parts, four
+// waves a quarter of the chunks each (the run of a frequent token goes over
+// hundreds), joined in order.  A workgroup has one chunk and 64 pieces of the row.
 template <typename TG>
 __global__ void __launch_bounds__(256)
 embedding_join_kernel(SumParams p, TG* __restrict__ dtable, int64_t ld) {
+  __shared__ float sum[3][8][64];
   const int64_t blk = block_id();
   if (blk >= p.blocks) return;
-  const int slices = (p.cv + p.cvs - 1) / p.cvs, teams = 256 / p.cvs;
-  const int slice = (int)(blk % slices), team = threadIdx.x / p.cvs, piece = slice * p.cvs + threadIdx.x % p.cvs;
-  const int64_t ch = blk / slices * teams + team;
-  if (team >= teams || piece >= p.cv || ch + 1 >= p.chunks) return;
+  const int slices = (p.cv + 63) / 64, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t ch = blk / slices;
+  const int piece = min((int)(blk % slices) * 64 + lane, p.cv - 1);
+  if (ch + 1 >= p.chunks) return;
   const int64_t s = ch * p.chunk, e = s + p.chunk;       // a chunk before the last is whole
   const uint32_t id = p.key[e - 1];
   if (id >= p.vocab || p.key[e] != id) return;           // nothing leaves
   if (s > 0 && p.key[s - 1] == id) return;               // it began before this chunk
-  float acc[8];
-  const float* d = p.part + ((ch * 2 + 1) * p.cv + piece) * kVE;
+  int64_t n = 0;                                         // chunks that begin with the run
+  for (;;) {
+    const int64_t x = ch + 1 + n + lane;
+    const uint64_t other = ~__ballot(x < p.chunks && p.key[min(x, p.chunks - 1) * p.chunk] == id);
+    if (other) {
+      n += __ffsll((unsigned long long)other) - 1;
+      break;
+    }
+    n += 64;
+  }
+  const int64_t lo = n * wave / 4, hi = n * (wave + 1) / 4;
+  const float* h = p.part + ((ch + 1) * 2 * p.cv + piece) * kVE;   // chunk x's part of the run that enters: + 2 x 8 cv
+  float acc[8] = {};
+  if (wave == 0) {
+    Row8<float> v;
+    v.load(p.part + ((ch * 2 + 1) * p.cv + piece) * kVE);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) acc[j] = d[j];
-  const float* h = p.part + piece * kVE;                   // chunk x's part of the run that enters: h + 2 x 8 cv
-  bool more = true;
-  for (int64_t x = ch + 1; more; x += kBatch) {
-    bool in[kBatch];
+    for (int j = 0; j < 8; ++j) acc[j] = v.v[j];
+  }
+  for (int64_t x = lo; x < hi; x += kBatch) {
     Row8<float> v[kBatch];
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      const int64_t y = min(x + u, p.chunks - 1);
-      in[u] = x + u < p.chunks && p.key[y * p.chunk] == id;   // sorted: once false, false from there on
-      v[u].load(h + y * 2 * p.cv * kVE);
-    }
+    for (int u = 0; u < kBatch; ++u) v[u].load(h + min(x + u, hi - 1) * 2 * p.cv * kVE);
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      if (!in[u]) {
-        more = false;
-        break;
-      }
+    for (int u = 0; u < kBatch; ++u)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] += v[u].v[j];
-    }
+      for (int j = 0; j < 8; ++j) acc[j] += x + u < hi ? v[u].v[j] : 0.f;
   }
+  if (wave > 0)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[wave - 1][j][lane] = acc[j];
+  __syncthreads();
+  if (wave > 0 || (int)(blk % slices) * 64 + lane >= p.cv) return;
+#pragma unroll
+  for (int w = 0; w < 3; ++w)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] += sum[w][j][lane];
   write_row(dtable, ld, id, piece * kVE, acc, p);
 }
 
@@ -514,7 +533,8 @@ hipError_t backward(const void* ids, int wide, int64_t rows, int64_t vocab, int 
     sp.row_out = (uint32_t*)(ws + pl.row[0]);
     sp.fill_hi = pieces;
     const int clear = (int)std::min<int64_t>((pieces + 15) / 16, 1024);
-    sort_small_kernel<<<1 + clear, 1024, 0, s>>>(sp);
+    if (rows <= 4096) sort_small_kernel<4><<<1 + clear, 1024, 0, s>>>(sp);
+    else sort_small_kernel<16><<<1 + clear, 1024, 0, s>>>(sp);
     if (hipError_t e = hipGetLastError()) return e;
   } else {
     last = (pl.passes - 1) & 1;
@@ -557,7 +577,8 @@ hipError_t backward(const void* ids, int wide, int64_t rows, int64_t vocab, int 
   q.blocks = (pl.chunks + teams - 1) / teams * slices;
   embedding_sum_kernel<TD, TG><<<folded_grid(q.blocks), 256, 0, s>>>(q, dy, ld_dy, dtable, ld);
   if (hipError_t e = hipGetLastError()) return e;
-  if (pl.chunks > 1) embedding_join_kernel<TG><<<folded_grid(q.blocks), 256, 0, s>>>(q, dtable, ld);
+  q.blocks = (pl.chunks - 1) * ((q.cv + 63) / 64);
+  if (q.blocks > 0) embedding_join_kernel<TG><<<folded_grid(q.blocks), 256, 0, s>>>(q, dtable, ld);
   return hipGetLastError();
 }
 

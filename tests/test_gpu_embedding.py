@@ -66,7 +66,7 @@ def test_gradient(td, tg, rows, vocab, c, wide, acc):
         assert np.array_equal(first, host(g))
 
 
-@pytest.mark.parametrize("rows,vocab,what", [(20000, 5, "few"), (20000, 70000, "many"), (12345, 600000, "one"),
+@pytest.mark.parametrize("rows,vocab,what", [(140000, 3, "few"), (16384, 300, "many"), (16385, 70000, "many"), (20000, 5, "few"), (20000, 70000, "many"), (12345, 600000, "one"),
                                              (20000, 9, "none"), (4096, 513, "each")])
 def test_gradient_runs(rows, vocab, what):
     """Runs over many chunks, three sort passes, all tokens equal, none inside."""
