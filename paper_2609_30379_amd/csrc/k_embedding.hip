@@ -91,14 +91,17 @@ embedding_kernel(const TT* __restrict__ table, int64_t ld_table, uint32_t vocab,
 }
 
 // ---------------------------------------------------------------- sort by id
-// Stable least-significant-digit radix sort of (id, row) pairs.  Up to kSmall
-// pairs are sorted by one workgroup in LDS, all passes in one launch.  More go
-// through two launches per pass: one counts the digits of every tile, the other
-// finds where a tile's pairs of each digit begin (all smaller digits, and the
-// same digit in the tiles before) and writes them there in their order.  The
-// gradient table is cleared meanwhile by further workgroups of the same launches:
-// the sort is short and latency-bound, the clearing long and bound by bytes.
-constexpr int kSmall = 16384, kSmallBits = 8, kMaxBins = 512;
+// Stable sort of (id, row) pairs.  Up to kSmall pairs take one launch: a workgroup
+// has a range of ids, looks at all tokens, keeps those in its range in LDS, counts
+// those below it (that is where its pairs go) and sorts what it kept by the few
+// bits that ids of one range differ in.  More pairs go through a least-significant-
+// digit radix sort of two launches per pass: one counts the digits of every tile,
+// the other finds where a tile's pairs of each digit begin (all smaller digits,
+// and the same digit in the tiles before) and writes them there in their order.
+// The gradient table is cleared meanwhile by further workgroups of the same
+// launches: the sort is short and latency-bound, the clearing long and bound by
+// bytes.
+constexpr int kSmall = 16384, kRanges = 128, kRangeBits = 8, kMaxBins = 512;
 
 struct SortParams {
   const void* ids;               // first pass: the tokens; later passes: NULL
@@ -108,7 +111,8 @@ struct SortParams {
   uint32_t *key_out, *row_out;
   uint32_t* hist;                // [tiles][bins]
   int64_t rows;
-  int tiles, shift, bits, passes;
+  int tiles, shift, bits, passes;   // tiles, or ranges of ids
+  uint32_t range;                // ids per range
   char* fill;                    // pieces fill_lo .. fill_hi of the gradient's memory are cleared, each fill_bytes long
   int64_t fill_ld, fill_lo, fill_hi, fill_total;   // and fill_ld apart; nothing past fill_total bytes
   int fill_bytes;
@@ -149,44 +153,71 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v, int lane) {      // in
 
 template <int ITER>
 __global__ void __launch_bounds__(1024)
-sort_small_kernel(SortParams p) {
-  constexpr int kPairs = ITER * 1024, kBins = 1 << kSmallBits;
-  __shared__ uint32_t keys[kPairs], wc[16][kBins], sums[4];
+sort_range_kernel(SortParams p) {
+  constexpr int kPairs = ITER * 1024, kBins = 1 << kRangeBits;
+  __shared__ uint32_t keys[kPairs], wc[16][kBins], sums[16], below_s[16];
   __shared__ uint16_t rows[kPairs];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  if (blockIdx.x > 0) {
-    clear_pieces(p, ((int64_t)blockIdx.x - 1) * 16 + wave, ((int64_t)gridDim.x - 1) * 16, lane);
+  if ((int)blockIdx.x >= p.tiles) {
+    clear_pieces(p, ((int64_t)blockIdx.x - p.tiles) * 16 + wave, ((int64_t)gridDim.x - p.tiles) * 16, lane);
     return;
   }
-  const int n = (int)p.rows, bins = 1 << p.bits, r0 = wave * (ITER * 64) + lane;
-  // wave w has a sixteenth of the pairs in order, 64 at a time
+  const uint32_t lo = blockIdx.x * p.range;
+  const int n_all = (int)p.rows, r0 = wave * (ITER * 64) + lane;
+  // wave w looks at a sixteenth of the tokens in order, 64 at a time
   uint32_t key[ITER], row[ITER], rank[ITER];
 #pragma unroll
   for (int k = 0; k < ITER; ++k) {
     const int r = r0 + k * 64;
-    key[k] = r < n ? token(p.ids, p.wide, r, p.vocab) : 0;
-    row[k] = r;
+    key[k] = r < n_all ? token(p.ids, p.wide, r, p.vocab) : 0xffffffffu;
   }
+  uint32_t inside = 0, below = 0;
+#pragma unroll
+  for (int k = 0; k < ITER; ++k) {
+    inside += __popcll(__ballot(key[k] - lo < p.range));
+    below += __popcll(__ballot(key[k] < lo));
+  }
+  if (lane == 0) {
+    sums[wave] = inside;
+    below_s[wave] = below;
+  }
+  __syncthreads();
+  uint32_t first = 0, n = 0, to0 = 0;                      // of all pairs, in this range, those of the waves before
+#pragma unroll
+  for (int w = 0; w < 16; ++w) {
+    first += below_s[w];
+    to0 += w < wave ? sums[w] : 0;
+    n += sums[w];
+  }
+  if (n == 0) return;
+#pragma unroll
+  for (int k = 0; k < ITER; ++k) {
+    const uint64_t in = __ballot(key[k] - lo < p.range);
+    if (key[k] - lo < p.range) {
+      const uint32_t to = to0 + lanes_below(in);
+      keys[to] = key[k] - lo;
+      rows[to] = (uint16_t)(r0 + k * 64);
+    }
+    to0 += __popcll(in);
+  }
+  // the range's pairs, again a sixteenth per wave
+  const int bins = 1 << p.bits, iters = ((int)n + 1023) / 1024, s0 = wave * (iters * 64) + lane;
   for (int pass = 0; pass < p.passes; ++pass) {
     const int shift = pass * p.bits;
-    if (pass > 0) {
-#pragma unroll
-      for (int k = 0; k < ITER; ++k) {
-        const int r = r0 + k * 64;
-        key[k] = r < n ? keys[r] : 0;
-        row[k] = r < n ? rows[r] : 0;
-      }
-    }
     for (int b = tid; b < 16 * kBins; b += 1024) (&wc[0][0])[b] = 0;
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < ITER; ++k) {
-      const bool ok = r0 + k * 64 < n;
+      if (k >= iters) break;
+      const int r = s0 + k * 64;
+      const bool ok = r < (int)n;
+      key[k] = ok ? keys[r] : 0;
+      row[k] = ok ? rows[r] : 0;
       const uint32_t dg = (key[k] >> shift) & (bins - 1);
       const uint64_t same = same_digit(dg, p.bits, __ballot(ok));
-      const uint32_t old = wc[wave][dg], below = lanes_below(same);
-      rank[k] = old + below;
-      if (ok && below == 0) wc[wave][dg] = old + __popcll(same);
+      const uint32_t old = wc[wave][dg], under = lanes_below(same);
+      rank[k] = old + under;
+      if (ok && under == 0) wc[wave][dg] = old + __popcll(same);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
     }
@@ -210,22 +241,21 @@ sort_small_kernel(SortParams p) {
       for (int w = 0; w < 16; ++w) wc[w][tid] += base;
     }
     __syncthreads();
+    const bool done = pass + 1 == p.passes;
 #pragma unroll
     for (int k = 0; k < ITER; ++k) {
-      if (r0 + k * 64 >= n) continue;
+      if (k >= iters) break;
+      if (s0 + k * 64 >= (int)n) continue;
       const uint32_t to = wc[wave][(key[k] >> shift) & (bins - 1)] + rank[k];
-      keys[to] = key[k];
-      rows[to] = (uint16_t)row[k];
+      if (done) {
+        p.key_out[first + to] = lo + key[k];
+        p.row_out[first + to] = row[k];
+      } else {
+        keys[to] = key[k];
+        rows[to] = (uint16_t)row[k];
+      }
     }
-    __syncthreads();
-  }
-#pragma unroll
-  for (int k = 0; k < ITER; ++k) {
-    const int r = tid + 1024 * k;
-    if (r < n) {
-      p.key_out[r] = keys[r];
-      p.row_out[r] = rows[r];
-    }
+    if (!done) __syncthreads();
   }
 }
 
@@ -479,16 +509,19 @@ int tile_iter(int64_t rows) { return rows <= 1 << 17 ? 4 : 16; }
 
 struct Plan {
   bool small;
+  int64_t range;
   int tiles, passes, bits, chunk, iter;
   int64_t chunks;
   size_t key[2], row[2], hist, part, bytes;
 };
 Plan plan(int64_t rows, int64_t vocab, int C) {
   Plan s{};
-  int bits = 1;
-  while ((vocab >> bits) > 0) ++bits;                    // ids 0 .. vocab
   s.small = rows <= kSmall;
-  const int most = s.small ? kSmallBits : 9;
+  s.range = s.small ? (vocab + kRanges) / kRanges : 0;   // ids 0 .. vocab in at most kRanges ranges
+  const int64_t top = s.small ? s.range - 1 : vocab;     // largest id that is sorted by
+  int bits = 1;
+  while ((top >> bits) > 0) ++bits;
+  const int most = s.small ? kRangeBits : 9;
   s.passes = (bits + most - 1) / most;
   s.bits = (bits + s.passes - 1) / s.passes;
   s.iter = tile_iter(rows);
@@ -533,8 +566,10 @@ hipError_t backward(const void* ids, int wide, int64_t rows, int64_t vocab, int 
     sp.row_out = (uint32_t*)(ws + pl.row[0]);
     sp.fill_hi = pieces;
     const int clear = (int)std::min<int64_t>((pieces + 15) / 16, 1024);
-    if (rows <= 4096) sort_small_kernel<4><<<1 + clear, 1024, 0, s>>>(sp);
-    else sort_small_kernel<16><<<1 + clear, 1024, 0, s>>>(sp);
+    sp.range = (uint32_t)pl.range;
+    sp.tiles = (int)((vocab + pl.range) / pl.range);
+    if (rows <= 4096) sort_range_kernel<4><<<sp.tiles + clear, 1024, 0, s>>>(sp);
+    else sort_range_kernel<16><<<sp.tiles + clear, 1024, 0, s>>>(sp);
     if (hipError_t e = hipGetLastError()) return e;
   } else {
     last = (pl.passes - 1) & 1;
