@@ -8,6 +8,7 @@
 // sum stay in two lanes and the weights P^T go from the accumulators of the
 // first product into the operand of the second without leaving the registers.
 #include <algorithm>
+#include <type_traits>
 
 #include "window_device.h"
 
@@ -104,7 +105,7 @@ template <typename T, int DP>
 __global__ void __launch_bounds__(256, DP == 128 ? (sizeof(T) == 4 ? 1 : 2) : DP == 64 && sizeof(T) == 4 ? 2 : 3)
 window_rows_kernel(WindowParams p) {
   typedef typename Frag<T>::type frag;
-  constexpr int KT = sizeof(T) == 2 ? 64 : 32, KB = KT / 32, NS = DP / 16, ND = DP / 32;
+  constexpr int KT = sizeof(T) == 2 ? 64 : 32, KB = KT / 32, NS = DP / 16, ND = DP / 32, kG = NS < 4 ? NS : 4;
   __shared__ __attribute__((aligned(16))) T Kb[2][KT * Tile<T, DP>::kLd];
   __shared__ __attribute__((aligned(16))) T Vb[2][KT * Tile<T, DP>::kLd];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h32 = lane >> 5;
@@ -154,61 +155,85 @@ window_rows_kernel(WindowParams p) {
   const KeyTiles kt(off + t0, off + t0 + (g0 + last) / p.group, m, p.left, p.right, p.sinks, KT);
   const T* kbase = (const T*)p.k + (int64_t)hk * p.d;
   const T* vbase = (const T*)p.v + (int64_t)hk * p.d;
-  Stage<T, DP, KT, 256> sk, sv;
-  auto load = [&](int tile) {
+  // The next tile's keys travel while the scores of this one are computed, its
+  // values while the weights are applied: one set of registers for both.
+  Stage<T, DP, KT, 256> stage;
+  auto load = [&](const T* base, int64_t ld, int tile) {
     const int j0 = kt.first(tile, KT), cnt = min(kt.end(tile) - j0, KT);
-    sk.load(tid, kbase + (int64_t)(k0 + j0) * p.ld_k, p.ld_k, cnt, p.d, p.narrow);
-    sv.load(tid, vbase + (int64_t)(k0 + j0) * p.ld_v, p.ld_v, cnt, p.d, p.narrow);
+    stage.load(tid, base + (int64_t)(k0 + j0) * ld, ld, cnt, p.d, p.narrow);
   };
   const int first = split * p.chunk, end = min(kt.n, first + p.chunk);
   if (first < end) {
-    load(first);
-    sk.store(tid, Kb[first & 1]);
-    sv.store(tid, Vb[first & 1]);
+    load(kbase, p.ld_k, first);
+    stage.store(tid, Kb[0]);
+    load(vbase, p.ld_v, first);
+    stage.store(tid, Vb[0]);
   }
-  for (int tile = first; tile < end; ++tile) {
+  // one tile from buffer B while the next one is on its way into the other: a
+  // constant, so that all LDS addresses of the loop are offsets of a few registers
+  auto body = [&](auto B, int tile) {
     __syncthreads();
-    const T *Ks = Kb[tile & 1], *Vs = Vb[tile & 1];
-    if (tile + 1 < end) load(tile + 1);
+    const T *Ks = Kb[B.value], *Vs = Vb[B.value];
+    if (tile + 1 < end) load(kbase, p.ld_k, tile + 1);
     const int j0 = kt.first(tile, KT), jend = kt.end(tile);
     // unless nothing of the tile is visible to any row of the wave
-    if (live && j0 <= hi_b && (min(j0 + KT, jend) > lo_a || j0 < p.sinks)) {
+    const bool seen = live && j0 <= hi_b && (min(j0 + KT, jend) > lo_a || j0 < p.sinks);
     const bool whole = j0 + KT <= jend && j0 + KT - 1 <= hi_a && (j0 >= lo_b || j0 + KT <= p.sinks);
+    // steps of at most four fragments, the reads of a step before the products of
+    // the one before
     f32x16 S[KB];
-    frag A[NS], X[ND], Y[ND];
-    read_along<DP>(Ks, 0, lane, A);
+    frag X[kG], Y[kG];
+    if (seen) {
+      read_part<DP, kG>(Ks, 0, 0, lane, X);
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      frag B[NS];
-      if (kb + 1 < KB) read_along<DP>(Ks, 32 * kb + 32, lane, B);
-      else read_across<DP>(Vs, 0, lane, tr, X);
-      pin();
-      S[kb] = product(A, Q);
-      pin();
-      if (kb + 1 < KB)
+      for (int kb = 0; kb < KB; ++kb) {
+        S[kb] = f32x16{};
+        if constexpr (NS > kG) {
+          read_part<DP, kG>(Ks, 32 * kb, kG, lane, Y);
+          pin();
+          S[kb] = product_part<kG>(X, Q, S[kb]);
+          pin();
+          if (kb + 1 < KB) read_part<DP, kG>(Ks, 32 * kb + 32, 0, lane, X);
+          pin();
+          S[kb] = product_part<kG>(Y, Q + kG, S[kb]);
+          pin();
+        } else {
+          if (kb + 1 < KB) read_part<DP, kG>(Ks, 32 * kb + 32, 0, lane, Y);
+          pin();
+          S[kb] = product_part<kG>(X, Q, S[kb]);
+          pin();
+          if (kb + 1 < KB)
 #pragma unroll
-        for (int ks = 0; ks < NS; ++ks) A[ks] = B[ks];
-    }
-    online_softmax<KB, ND>(S, O, mx, l, p.c, whole, j0, jend, lo, hi, p.sinks, h32);
-    pin();
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      frag P;
-      read_across<DP>(Vs, 32 * kb + 16, lane, tr, Y);
-      to_operand(S[kb], 0, P);
-      pin();
-      add_products(X, P, O);
-      to_operand(S[kb], 1, P);
-      pin();
-      if (kb + 1 < KB) read_across<DP>(Vs, 32 * kb + 32, lane, tr, X);
-      pin();
-      add_products(Y, P, O);
-    }
+            for (int k = 0; k < kG; ++k) X[k] = Y[k];
+        }
+      }
+      online_softmax<KB, ND>(S, O, mx, l, p.c, whole, j0, jend, lo, hi, p.sinks, h32);
     }
     if (tile + 1 < end) {
-      sk.store(tid, Kb[~tile & 1]);
-      sv.store(tid, Vb[~tile & 1]);
+      stage.store(tid, Kb[1 - B.value]);
+      load(vbase, p.ld_v, tile + 1);
     }
+    if (seen) {
+      read_across<DP>(Vs, 0, lane, tr, X);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        frag P;
+        read_across<DP>(Vs, 32 * kb + 16, lane, tr, Y);
+        to_operand(S[kb], 0, P);
+        pin();
+        add_products(X, P, O);
+        to_operand(S[kb], 1, P);
+        pin();
+        if (kb + 1 < KB) read_across<DP>(Vs, 32 * kb + 32, lane, tr, X);
+        pin();
+        add_products(Y, P, O);
+      }
+    }
+    if (tile + 1 < end) stage.store(tid, Vb[1 - B.value]);
+  };
+  for (int tile = first; tile < end; tile += 2) {
+    body(std::integral_constant<int, 0>{}, tile);
+    if (tile + 1 < end) body(std::integral_constant<int, 1>{}, tile + 1);
   }
 
   if (wave * 32 + (lane & 31) > last) return;

@@ -36,17 +36,52 @@ struct WindowBwdParams {
   float *sink_part, *sink_sum;   // [batch][kv_heads][subs][pieces][2][32][DP], [batch][kv_heads][subs][2][32][DP]
 };
 
+// At most so many blocks of 128 rows, or of 128 keys, of all heads: blocks of 32 instead.
+constexpr int kFewRowBlocks = 128, kFewKeyBlocks = 256;
+
 // First query past the window of the keys jb .. jl; the queries before it are
 // gone through by the keys' own workgroup.
 __device__ __forceinline__ int window_end(int jl, int left, int off, int n) { return min(n, max(0, jl + left - off + 1)); }
 
-constexpr int kBlockShift = 7;
+constexpr int kBlockShift = 7, kFewShift = 5;   // rows or keys per workgroup: four waves x 32, or 32 in all
+
+// A row's q and dout as operands, and D.
+template <typename T, int DP>
+__device__ __forceinline__ void load_row(const WindowBwdParams& p, int64_t token, int head, int h32,
+                                         typename Frag<T>::type (&Q)[DP / 16], typename Frag<T>::type (&G)[DP / 16],
+                                         float& delta) {
+  typedef typename Frag<T>::type frag;
+  const T* src = (const T*)p.q + token * p.ld_q + (int64_t)head * p.d;
+  const T* dsrc = (const T*)p.dout + token * p.ld_dout + (int64_t)head * p.d;
+  const T* osrc = (const T*)p.o + token * p.ld_o + (int64_t)head * p.d;
+#pragma unroll
+  for (int ks = 0; ks < DP / 16; ++ks) {
+    const int e = 16 * ks + 8 * h32;
+    frag z = {}, o = {};
+    Q[ks] = e < p.d ? *reinterpret_cast<const frag*>(src + e) : z;
+    G[ks] = e < p.d ? *reinterpret_cast<const frag*>(dsrc + e) : z;
+    if (e < p.d) o = *reinterpret_cast<const frag*>(osrc + e);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) delta = fmaf((float)o[u], (float)G[ks][u], delta);
+  }
+  delta = pair_sum(delta);
+  multiply<T>(Q, p.qmul);
+}
+// Four channels of dq, rounded once.
+template <typename T>
+__device__ __forceinline__ void write_row(const WindowBwdParams& p, int64_t token, int head, int at, const f32x4& dq) {
+  typedef T vec4 __attribute__((ext_vector_type(4)));
+  vec4 w;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) w[u] = (T)(dq[u] * p.scale);
+  *reinterpret_cast<vec4*>((T*)p.dq + token * p.ld_dq + (int64_t)head * p.d + at) = w;
+}
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(256, DP == 32 ? 3 : DP == 128 ? 1 : 2)
+__global__ void __launch_bounds__(256, DP == 32 ? 3 : DP == 128 && sizeof(T) == 4 ? 1 : 2)
 window_dq_kernel(WindowBwdParams p) {
   typedef typename Frag<T>::type frag;
-  constexpr int KT = sizeof(T) == 2 ? 64 : 32, KB = KT / 32, NS = DP / 16, ND = DP / 32;
+  constexpr int KT = sizeof(T) == 2 ? 64 : 32, KB = KT / 32, NS = DP / 16, ND = DP / 32, kG = NS < 4 ? NS : 4;
   __shared__ __attribute__((aligned(16))) T Kb[2][KT * Tile<T, DP>::kLd];
   __shared__ __attribute__((aligned(16))) T Vb[2][KT * Tile<T, DP>::kLd];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h32 = lane >> 5;
@@ -70,23 +105,7 @@ window_dq_kernel(WindowBwdParams p) {
 
   frag Q[NS], G[NS];
   float delta = 0.f;
-  {
-    const T* src = (const T*)p.q + (int64_t)(q0 + t) * p.ld_q + (int64_t)head * p.d;
-    const T* dsrc = (const T*)p.dout + (int64_t)(q0 + t) * p.ld_dout + (int64_t)head * p.d;
-    const T* osrc = (const T*)p.o + (int64_t)(q0 + t) * p.ld_o + (int64_t)head * p.d;
-#pragma unroll
-    for (int ks = 0; ks < NS; ++ks) {
-      const int e = 16 * ks + 8 * h32;
-      frag z = {}, o = {};
-      Q[ks] = e < p.d ? *reinterpret_cast<const frag*>(src + e) : z;
-      G[ks] = e < p.d ? *reinterpret_cast<const frag*>(dsrc + e) : z;
-      if (e < p.d) o = *reinterpret_cast<const frag*>(osrc + e);
-#pragma unroll
-      for (int u = 0; u < 8; ++u) delta = fmaf((float)o[u], (float)G[ks][u], delta);
-    }
-    delta = pair_sum(delta);
-    multiply<T>(Q, p.qmul);
-  }
+  load_row<T, DP>(p, q0 + t, head, h32, Q, G, delta);
   const float lse = p.lse[(int64_t)head * p.ld_lse + q0 + t], nlse2 = lse == -INFINITY ? 0.f : -lse * kLog2e;
   if (mine && h32 == 0) p.delta[(int64_t)head * p.sum_q + q0 + t] = delta;
   uint32_t tr[2];
@@ -99,30 +118,34 @@ window_dq_kernel(WindowBwdParams p) {
   const KeyTiles kt(off + t0, off + t0 + (g0 + last) / p.group, m, p.left, p.right, p.sinks, KT);
   const T* kbase = (const T*)p.k + (int64_t)hk * p.d;
   const T* vbase = (const T*)p.v + (int64_t)hk * p.d;
-  Stage<T, DP, KT, 256> sk, sv;
-  auto load = [&](int tile) {
+  // the next tile's keys travel during the first half of this one, its values
+  // during the second: one set of registers for both
+  Stage<T, DP, KT, 256> stage;
+  auto load = [&](const T* base, int64_t ld, int tile) {
     const int j0 = kt.first(tile, KT), cnt = min(kt.end(tile) - j0, KT);
-    sk.load(tid, kbase + (int64_t)(k0 + j0) * p.ld_k, p.ld_k, cnt, p.d, p.narrow);
-    sv.load(tid, vbase + (int64_t)(k0 + j0) * p.ld_v, p.ld_v, cnt, p.d, p.narrow);
+    stage.load(tid, base + (int64_t)(k0 + j0) * ld, ld, cnt, p.d, p.narrow);
   };
   if (kt.n > 0) {
-    load(0);
-    sk.store(tid, Kb[0]);
-    sv.store(tid, Vb[0]);
+    load(kbase, p.ld_k, 0);
+    stage.store(tid, Kb[0]);
+    load(vbase, p.ld_v, 0);
+    stage.store(tid, Vb[0]);
   }
-  for (int tile = 0; tile < kt.n; ++tile) {
+  auto body = [&](auto B, int tile) {                      // one tile from buffer B, a constant
     __syncthreads();
-    const T *Ks = Kb[tile & 1], *Vs = Vb[tile & 1];
-    if (tile + 1 < kt.n) load(tile + 1);
+    const T *Ks = Kb[B.value], *Vs = Vb[B.value];
+    if (tile + 1 < kt.n) load(kbase, p.ld_k, tile + 1);
     const int j0 = kt.first(tile, KT), jend = kt.end(tile);
-    if (live && j0 <= hi_b && (min(j0 + KT, jend) > lo_a || j0 < p.sinks)) {
+    const bool seen = live && j0 <= hi_b && (min(j0 + KT, jend) > lo_a || j0 < p.sinks);
     const bool whole = j0 + KT <= jend && j0 + KT - 1 <= hi_a && (j0 >= lo_b || j0 + KT <= p.sinks);
-    // Block by block of 32 keys, the reads of a step before the products of the
-    // one before; a hidden pair's score starts from -inf, dP from -D.
-    frag A[NS], B[NS], X[ND], Y[ND];
-    read_along<DP>(Ks, 0, lane, A);
+    // Block by block of 32 keys in steps of at most four fragments, the reads of a
+    // step before the products of the one before; a hidden pair's score starts
+    // from -inf, dP from -D.
+    frag X[kG], Y[kG];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
+      if (seen) {
+      read_part<DP, kG>(Ks, 32 * kb, 0, lane, X);
       f32x16 S = f32x16{}, dP;
       if (!whole) {
 #pragma unroll
@@ -133,99 +156,354 @@ window_dq_kernel(WindowBwdParams p) {
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) dP[e] = -delta;
-      pin();
-      read_along<DP>(Vs, 32 * kb, lane, B);
-      pin();
-      S = product(A, Q, S);
-      pin();
-      read_across<DP>(Ks, 32 * kb, lane, tr, X);
-      pin();
-      dP = product(B, G, dP);
+      if constexpr (NS > kG) {
+        read_part<DP, kG>(Ks, 32 * kb, kG, lane, Y);
+        S = product_part<kG>(X, Q, S);
+        read_part<DP, kG>(Vs, 32 * kb, 0, lane, X);
+        S = product_part<kG>(Y, Q + kG, S);
+        read_part<DP, kG>(Vs, 32 * kb, kG, lane, Y);
+        dP = product_part<kG>(X, G, dP);
+        read_across<DP>(Ks, 32 * kb, lane, tr, X);
+        dP = product_part<kG>(Y, G + kG, dP);
+      } else {
+        read_part<DP, kG>(Vs, 32 * kb, 0, lane, Y);
+        S = product_part<kG>(X, Q, S);
+        read_across<DP>(Ks, 32 * kb, lane, tr, X);
+        dP = product_part<kG>(Y, G, dP);
+      }
 #pragma unroll
       for (int e = 0; e < 16; ++e) S[e] = __builtin_amdgcn_exp2f(fmaf(S[e], p.c, nlse2));
-      pin();
       read_across<DP>(Ks, 32 * kb + 16, lane, tr, Y);
-      pin();
 #pragma unroll
       for (int e = 0; e < 16; ++e) S[e] *= dP[e];
       frag D;
       to_operand(S, 0, D);
       add_products(X, D, dQ);
       to_operand(S, 1, D);
-      pin();
-      if (kb + 1 < KB) read_along<DP>(Ks, 32 * kb + 32, lane, A);
-      pin();
       add_products(Y, D, dQ);
+      }
+      if (kb == (KB - 1) / 2 && tile + 1 < kt.n) {
+        stage.store(tid, Kb[1 - B.value]);
+        load(vbase, p.ld_v, tile + 1);
+      }
     }
-    }
-    if (tile + 1 < kt.n) {
-      sk.store(tid, Kb[~tile & 1]);
-      sv.store(tid, Vb[~tile & 1]);
-    }
+    if (tile + 1 < kt.n) stage.store(tid, Vb[1 - B.value]);
+  };
+  for (int tile = 0; tile < kt.n; tile += 2) {
+    body(std::integral_constant<int, 0>{}, tile);
+    if (tile + 1 < kt.n) body(std::integral_constant<int, 1>{}, tile + 1);
   }
   if (!mine) return;
-  T* dst = (T*)p.dq + (int64_t)(q0 + t) * p.ld_dq + (int64_t)head * p.d;
 #pragma unroll
   for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
     for (int e = 0; e < 16; e += 4) {
       const int at = 32 * dt + 2 * e + 4 * h32;
-      if (at < p.d) {
-        typedef T vec4 __attribute__((ext_vector_type(4)));
-        vec4 w;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) w[u] = (T)(dQ[dt][e + u] * p.scale);
-        *reinterpret_cast<vec4*>(dst + at) = w;
-      }
+      if (at < p.d) write_row<T>(p, q0 + t, head, at, f32x4{dQ[dt][e], dQ[dt][e + 1], dQ[dt][e + 2], dQ[dt][e + 3]});
     }
 }
 
+// dQ of 32 rows per workgroup, its four waves on different key tiles, each with its
+// own tile in LDS, their sums joined in order at the end: for calls whose blocks of
+// 128 rows would leave most of the card idle.
+template <typename T, int DP>
+__global__ void __launch_bounds__(256, DP == 128 || (DP == 64 && sizeof(T) == 4) ? 1 : 2)
+window_dq_few_kernel(WindowBwdParams p) {
+  typedef typename Frag<T>::type frag;
+  constexpr int KT = 32, NS = DP / 16, ND = DP / 32, kOutLd = DP + 4;
+  union Shared {
+    T tile[4][2][KT * Tile<T, DP>::kLd];
+    float sum[4][32 * kOutLd];
+  };
+  __shared__ __attribute__((aligned(16))) Shared sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h32 = lane >> 5;
+  const int64_t item = block_id();
+  if (item >= p.items) return;
+  const int hk = (int)(item % p.kv_heads);
+  const int64_t b = item / p.kv_heads;
+  const int i = find_sample(p.cu_q, p.batch, p.group, kFewShift, b, lane);
+  const int q0 = p.cu_q[i], n = p.cu_q[i + 1] - q0, k0 = p.cu_k[i], m = p.cu_k[i + 1] - k0;
+  const int64_t rows = (int64_t)n * p.group, r0 = (b - block_start(p.cu_q, i, p.group, kFewShift)) << kFewShift;
+  if (r0 >= rows) return;
+  const int t0 = (int)(r0 / p.group), g0 = (int)(r0 - (int64_t)t0 * p.group);
+  const int last = (int)min((int64_t)31, rows - 1 - r0), off = m - n;
+  const int x = min(lane & 31, last), tg = div_group(g0 + x, p.inv_group);
+  const int t = t0 + tg, g = g0 + x - tg * p.group, pos = off + t, head = hk * p.group + g;
+  const int lo = p.left >= 0 ? pos - p.left : 0, hi = p.right >= 0 ? min(pos + p.right, m - 1) : m - 1;
+  const int pos_a = off + t0, pos_b = off + t0 + (g0 + last) / p.group;
+  const int hi_a = p.right >= 0 ? min(pos_a + p.right, m - 1) : m - 1, lo_b = p.left >= 0 ? pos_b - p.left : 0;
+
+  const KeyTiles kt(pos_a, pos_b, m, p.left, p.right, p.sinks, KT);
+  const T* kbase = (const T*)p.k + (int64_t)hk * p.d;
+  const T* vbase = (const T*)p.v + (int64_t)hk * p.d;
+  Stage<T, DP, KT, 64> sk, sv;
+  auto load = [&](int tile) {
+    const int j0 = kt.first(tile, KT), cnt = min(kt.end(tile) - j0, KT);
+    sk.load(lane, kbase + (int64_t)(k0 + j0) * p.ld_k, p.ld_k, cnt, p.d, p.narrow);
+    sv.load(lane, vbase + (int64_t)(k0 + j0) * p.ld_v, p.ld_v, cnt, p.d, p.narrow);
+  };
+  if (wave < kt.n) load(wave);
+  frag Q[NS], G[NS];
+  float delta = 0.f;
+  load_row<T, DP>(p, q0 + t, head, h32, Q, G, delta);
+  const float lse = p.lse[(int64_t)head * p.ld_lse + q0 + t], nlse2 = lse == -INFINITY ? 0.f : -lse * kLog2e;
+  if (wave == 0 && h32 == 0 && (lane & 31) <= last) p.delta[(int64_t)head * p.sum_q + q0 + t] = delta;
+  uint32_t tr[2];
+  Tile<T, DP>::across_addr(lane, tr);
+  f32x16 dQ[ND];
+#pragma unroll
+  for (int dt = 0; dt < ND; ++dt) dQ[dt] = f32x16{};
+  T *Ks = sh.tile[wave][0], *Vs = sh.tile[wave][1];
+  auto own = [] {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+  for (int tile = wave; tile < kt.n; tile += 4) {
+    own();
+    sk.store(lane, Ks);
+    sv.store(lane, Vs);
+    own();
+    if (tile + 4 < kt.n) load(tile + 4);
+    const int j0 = kt.first(tile, KT), jend = kt.end(tile);
+    const bool whole = j0 + KT <= jend && j0 + KT - 1 <= hi_a && (j0 >= lo_b || j0 + KT <= p.sinks);
+    f32x16 S = f32x16{}, dP;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int j = j0 + 8 * (e >> 2) + 4 * h32 + (e & 3);
+      if (!whole) S[e] = j < jend && j <= hi && (j >= lo || j < p.sinks) ? 0.f : -INFINITY;
+      dP[e] = -delta;
+    }
+    frag A[NS], X[ND], D;
+    read_along<DP>(Ks, 0, lane, A);
+    S = product(A, Q, S);
+    read_along<DP>(Vs, 0, lane, A);
+    dP = product(A, G, dP);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) S[e] = __builtin_amdgcn_exp2f(fmaf(S[e], p.c, nlse2)) * dP[e];
+#pragma unroll
+    for (int nn = 0; nn < 2; ++nn) {
+      read_across<DP>(Ks, 16 * nn, lane, tr, X);
+      to_operand(S, nn, D);
+      add_products(X, D, dQ);
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4)
+      *reinterpret_cast<f32x4*>(&sh.sum[wave][(lane & 31) * kOutLd + 32 * dt + 2 * e + 4 * h32]) =
+          f32x4{dQ[dt][e], dQ[dt][e + 1], dQ[dt][e + 2], dQ[dt][e + 3]};
+  __syncthreads();
+  for (int u = tid; u < (last + 1) * (DP / 4); u += 256) {
+    const int r = u / (DP / 4), at = u % (DP / 4) * 4;
+    f32x4 a = *reinterpret_cast<f32x4*>(&sh.sum[0][r * kOutLd + at]);
+#pragma unroll
+    for (int w = 1; w < 4; ++w) a += *reinterpret_cast<f32x4*>(&sh.sum[w][r * kOutLd + at]);
+    if (at >= p.d) continue;
+    const int rt = div_group(g0 + r, p.inv_group);
+    write_row<T>(p, q0 + t0 + rt, hk * p.group + g0 + r - rt * p.group, at, a);
+  }
+}
+
+// One block of 32 rows (in LDS from row r0) against the wave's 32 keys, in steps of
+// at most four fragments: each step issues the reads of the next one before its
+// products, and the exponentials and score gradients run under products.  lse_s
+// holds -lse log2(e) (-inf for a row past the end: weight 0), delta_s -D, pos_s the
+// rows' positions; a hidden pair's score starts from -inf.
+template <typename T, int DP>
+__device__ __forceinline__ void key_block(const T* Qs, const T* Gs, const float* lse_s, const float* delta_s,
+                                          const int* pos_s, int r0, bool whole, int plo, int phi, float c,
+                                          const typename Frag<T>::type (&K)[DP / 16],
+                                          const typename Frag<T>::type (&V)[DP / 16], f32x16 (&dK)[DP / 32],
+                                          f32x16 (&dV)[DP / 32], int lane, const uint32_t (&tr)[2]) {
+  typedef typename Frag<T>::type frag;
+  constexpr int NS = DP / 16, ND = DP / 32, kG = NS < 4 ? NS : 4;
+  const int h32 = lane >> 5;
+  frag X[kG], Y[kG], W;
+  read_part<DP, kG>(Qs, r0, 0, lane, X);
+  f32x16 S = f32x16{}, dP;
+  if (!whole) {
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+      const int4 ps = *reinterpret_cast<const int4*>(pos_s + r0 + 8 * e4 + 4 * h32);
+      const int pr[4] = {ps.x, ps.y, ps.z, ps.w};
+#pragma unroll
+      for (int u = 0; u < 4; ++u) S[4 * e4 + u] = pr[u] >= plo && pr[u] <= phi ? 0.f : -INFINITY;
+    }
+  }
+  pin();
+  if constexpr (NS > kG) {
+    read_part<DP, kG>(Qs, r0, kG, lane, Y);
+    pin();
+    S = product_part<kG>(X, K, S);
+    pin();
+    read_part<DP, kG>(Gs, r0, 0, lane, X);
+    pin();
+    S = product_part<kG>(Y, K + kG, S);
+    pin();
+  } else {
+    read_part<DP, kG>(Gs, r0, 0, lane, Y);
+    pin();
+    S = product_part<kG>(X, K, S);
+    pin();
+#pragma unroll
+    for (int k = 0; k < kG; ++k) X[k] = Y[k];
+  }
+#pragma unroll
+  for (int e4 = 0; e4 < 4; ++e4) {
+    const f32x4 de = *reinterpret_cast<const f32x4*>(delta_s + r0 + 8 * e4 + 4 * h32);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) dP[4 * e4 + u] = de[u];
+  }
+  if constexpr (NS > kG) {
+    read_part<DP, kG>(Gs, r0, kG, lane, Y);
+    pin();
+    dP = product_part<kG>(X, V, dP);
+    pin();
+    read_across<DP>(Gs, r0, lane, tr, X);
+    pin();
+    dP = product_part<kG>(Y, V + kG, dP);
+  } else {
+    read_across<DP>(Gs, r0, lane, tr, Y);
+    pin();
+    dP = product_part<kG>(X, V, dP);
+#pragma unroll
+    for (int k = 0; k < ND; ++k) X[k] = Y[k];
+  }
+#pragma unroll
+  for (int e4 = 0; e4 < 4; ++e4) {
+    const f32x4 ls = *reinterpret_cast<const f32x4*>(lse_s + r0 + 8 * e4 + 4 * h32);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) S[4 * e4 + u] = __builtin_amdgcn_exp2f(fmaf(S[4 * e4 + u], c, ls[u]));
+  }
+  to_operand(S, 0, W);
+  pin();
+  read_across<DP>(Gs, r0 + 16, lane, tr, Y);
+  pin();
+  add_products(X, W, dV);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) dP[e] *= S[e];
+  to_operand(S, 1, W);
+  pin();
+  read_across<DP>(Qs, r0, lane, tr, X);
+  pin();
+  add_products(Y, W, dV);
+  to_operand(dP, 0, W);
+  pin();
+  read_across<DP>(Qs, r0 + 16, lane, tr, Y);
+  pin();
+  add_products(X, W, dK);
+  to_operand(dP, 1, W);
+  pin();
+  add_products(Y, W, dK);
+}
+
+// Positions of the rows that see a key: plo .. phi.
+__device__ __forceinline__ int first_seeing(const WindowBwdParams& p, int j) {
+  return p.right >= 0 ? j - p.right : INT32_MIN + 1;
+}
+__device__ __forceinline__ int last_seeing(const WindowBwdParams& p, int j) {
+  return p.left >= 0 && j >= p.sinks ? j + p.left : INT32_MAX;
+}
+// The same for all keys ja .. je: first of the last key, last of the first key that is no sink.
+__device__ __forceinline__ int last_seeing_all(const WindowBwdParams& p, int ja, int je) {
+  return p.left >= 0 && je >= p.sinks ? max(ja, p.sinks) + p.left : INT32_MAX;
+}
+
+template <typename T, int DP>
+__device__ __forceinline__ void load_keys(const WindowBwdParams& p, int64_t row, int hk, int h32,
+                                          typename Frag<T>::type (&K)[DP / 16], typename Frag<T>::type (&V)[DP / 16]) {
+  typedef typename Frag<T>::type frag;
+  const T* ksrc = (const T*)p.k + row * p.ld_k + (int64_t)hk * p.d;
+  const T* vsrc = (const T*)p.v + row * p.ld_v + (int64_t)hk * p.d;
+#pragma unroll
+  for (int ks = 0; ks < DP / 16; ++ks) {
+    const int e = 16 * ks + 8 * h32;
+    frag z = {};
+    K[ks] = e < p.d ? *reinterpret_cast<const frag*>(ksrc + e) : z;
+    V[ks] = e < p.d ? *reinterpret_cast<const frag*>(vsrc + e) : z;
+  }
+  multiply<T>(K, p.qmul);
+}
+
+// Four channels of dk and dv of a key (the row of the packed keys), rounded once.
+template <typename T>
+__device__ __forceinline__ void write_keys(const WindowBwdParams& p, int64_t row, int hk, int at, const f32x4& dk,
+                                           const f32x4& dv) {
+  typedef T vec4 __attribute__((ext_vector_type(4)));
+  vec4 a, w;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    a[u] = (T)(dk[u] * p.scale);
+    w[u] = (T)dv[u];
+  }
+  *reinterpret_cast<vec4*>((T*)p.dk + row * p.ld_dk + (int64_t)hk * p.d + at) = a;
+  *reinterpret_cast<vec4*>((T*)p.dv + row * p.ld_dv + (int64_t)hk * p.d + at) = w;
+}
+
+// The rows of a tile on their way into LDS: q and dout of all query heads that
+// share the keys, and the rows' statistics.  THREADS threads of index tid.
+template <typename T, int DP, int RT, int THREADS> struct RowTile {
+  Stage<T, DP, RT, THREADS> q, g;
+  float lse, delta;
+  int pos;
+  // cnt rows from row g0 of query t0 of the sample that begins at q0
+  __device__ __forceinline__ void load(const WindowBwdParams& p, int tid, int hk, int q0, int t0, int g0, int queries,
+                                       int cnt, int off) {
+    const int first = q0 + t0, h0 = hk * p.group;
+    q.load_group(tid, (const T*)p.q + (int64_t)first * p.ld_q + (int64_t)h0 * p.d, p.ld_q, queries, g0, p.group,
+                 p.inv_group, p.d, p.narrow);
+    g.load_group(tid, (const T*)p.dout + (int64_t)first * p.ld_dout + (int64_t)h0 * p.d, p.ld_dout, queries, g0, p.group,
+                 p.inv_group, p.d, p.narrow);
+    if (tid < RT) {
+      const int r = min(tid, cnt - 1), tg = div_group(g0 + r, p.inv_group), head = h0 + g0 + r - tg * p.group;
+      lse = p.lse[(int64_t)head * p.ld_lse + first + tg];
+      delta = p.delta[(int64_t)head * p.sum_q + first + tg];
+      pos = off + t0 + tg;
+      if (tid >= cnt) lse = INFINITY;
+    }
+  }
+  __device__ __forceinline__ void store(int tid, T* qs, T* gs, float* lse_s, float* delta_s, int* pos_s) const {
+    q.store(tid, qs);
+    g.store(tid, gs);
+    if (tid < RT) {
+      lse_s[tid] = lse == -INFINITY ? 0.f : lse * -kLog2e;   // -inf: a row that sees nothing, hidden everywhere
+      delta_s[tid] = -delta;
+      pos_s[tid] = pos;
+    }
+  }
+};
+
+// dK and dV of 128 keys, 32 per wave; the workgroup walks the rows that see them.
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, DP == 128 || (DP == 64 && sizeof(T) == 4) ? 1 : 2)
 window_dkv_kernel(WindowBwdParams p) {
   typedef typename Frag<T>::type frag;
-  constexpr int RT = sizeof(T) == 2 ? 64 : 32, RB = RT / 32, NS = DP / 16, ND = DP / 32;
-  __shared__ __attribute__((aligned(16))) T Qb[2][RT * Tile<T, DP>::kLd];
-  __shared__ __attribute__((aligned(16))) T Gb[2][RT * Tile<T, DP>::kLd];
-  __shared__ __attribute__((aligned(16))) float lse_b[2][RT];
-  __shared__ __attribute__((aligned(16))) float delta_b[2][RT];
-  __shared__ __attribute__((aligned(16))) int pos_b[2][RT];
+  constexpr int RT = sizeof(T) == 2 ? 64 : 32, ND = DP / 32;
+  __shared__ __attribute__((aligned(16))) T Qs[RT * Tile<T, DP>::kLd];
+  __shared__ __attribute__((aligned(16))) T Gs[RT * Tile<T, DP>::kLd];
+  __shared__ __attribute__((aligned(16))) float lse_s[RT];
+  __shared__ __attribute__((aligned(16))) float delta_s[RT];
+  __shared__ __attribute__((aligned(16))) int pos_s[RT];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h32 = lane >> 5;
   const int64_t item = block_id();
   if (item >= p.items) return;
   const int hk = (int)(item % p.kv_heads);
   const int64_t b = item / p.kv_heads;
   const int i = find_sample(p.cu_k, p.batch, 1, kBlockShift, b, lane);
-  const int q0 = p.cu_q[i], n = p.cu_q[i + 1] - q0, k0 = p.cu_k[i], m = p.cu_k[i + 1] - k0;
+  const int q0 = p.cu_q[i], n = p.cu_q[i + 1] - q0, k0 = p.cu_k[i], m = p.cu_k[i + 1] - k0, off = m - n;
   const int64_t jb64 = (b - block_start(p.cu_k, i, 1, kBlockShift)) << kBlockShift;
   if (jb64 >= m) return;
   const int jb = (int)jb64, jl = min(jb + 127, m - 1);          // keys jb .. jl
-  const int off = m - n;
   const int j = min(jb + wave * 32 + (lane & 31), m - 1);       // a lane past the last key takes the last one, not stored
   const bool live = jb + wave * 32 < m, mine = jb + wave * 32 + (lane & 31) < m;
-  // positions of the rows that see key j
-  const int plo = p.right >= 0 ? j - p.right : INT32_MIN + 1;
-  const int phi = p.left >= 0 && j >= p.sinks ? j + p.left : INT32_MAX;
-
-  // the same bounds over the wave's keys
-  const int ja = min(jb + wave * 32, m - 1), je = min(jb + wave * 32 + 31, m - 1);
-  const int plo_a = p.right >= 0 ? ja - p.right : INT32_MIN + 1, plo_b = p.right >= 0 ? je - p.right : INT32_MIN + 1;
-  const int phi_a = p.left >= 0 && je >= p.sinks ? max(ja, p.sinks) + p.left : INT32_MAX;
+  const int plo = first_seeing(p, j), phi = last_seeing(p, j);
+  const int ja = min(jb + wave * 32, m - 1), je = min(jb + wave * 32 + 31, m - 1);      // the wave's keys
+  const int plo_a = first_seeing(p, ja), plo_b = first_seeing(p, je), phi_a = last_seeing_all(p, ja, je);
   const int phi_b = p.left >= 0 && ja >= p.sinks ? je + p.left : INT32_MAX;
-
-  frag K[NS], V[NS];
-  {
-    const T* ksrc = (const T*)p.k + (int64_t)(k0 + j) * p.ld_k + (int64_t)hk * p.d;
-    const T* vsrc = (const T*)p.v + (int64_t)(k0 + j) * p.ld_v + (int64_t)hk * p.d;
-#pragma unroll
-    for (int ks = 0; ks < NS; ++ks) {
-      const int e = 16 * ks + 8 * h32;
-      frag z = {};
-      K[ks] = e < p.d ? *reinterpret_cast<const frag*>(ksrc + e) : z;
-      V[ks] = e < p.d ? *reinterpret_cast<const frag*>(vsrc + e) : z;
-    }
-    multiply<T>(K, p.qmul);
-  }
+  frag K[DP / 16], V[DP / 16];
+  load_keys<T, DP>(p, k0 + j, hk, h32, K, V);
   uint32_t tr[2];
   Tile<T, DP>::across_addr(lane, tr);
   f32x16 dK[ND], dV[ND];
@@ -234,289 +512,185 @@ window_dkv_kernel(WindowBwdParams p) {
 
   // queries that see a key of the block, as rows [ra, rb)
   const int ta = p.right >= 0 ? min(max(0, jb - p.right - off), n) : 0;
-  const int tb = p.left >= 0 && (jb >= p.sinks || p.split) ? window_end(jl, p.left, off, n) : n;
-  const int64_t ra = (int64_t)ta * p.group, rb = (int64_t)max(ta, tb) * p.group;
-  const int tiles = (int)((rb - ra + RT - 1) / RT);
-  Stage<T, DP, RT, 256> sq, sg;
-  float r_lse = 0.f, r_delta = 0.f;
-  int r_pos = 0;
-  // the tile's first row as (t0, g0), moved on by RT rows per tile
+  const int tb = max(ta, p.left >= 0 && (jb >= p.sinks || p.split) ? window_end(jl, p.left, off, n) : n);
+  const int64_t rows = (int64_t)(tb - ta) * p.group;
+  const int tiles = (int)((rows + RT - 1) / RT);
+  RowTile<T, DP, RT, 256> in;
+  // a tile's first row as (t0, g0), moved on by RT rows per tile
   const int step_t = RT / p.group, step_g = RT - step_t * p.group;
-  int lt0 = ta, lg0 = 0;
-  int64_t left_rows = rb - ra;
-  auto load = [&]() {
-    const int cnt = (int)min((int64_t)RT, left_rows), queries = min(tb - lt0, RT + 1);
-    const int first = q0 + lt0, h0 = hk * p.group;
-    sq.load_group(tid, (const T*)p.q + (int64_t)first * p.ld_q + (int64_t)h0 * p.d, p.ld_q, queries, lg0, p.group,
-                  p.inv_group, p.d, p.narrow);
-    sg.load_group(tid, (const T*)p.dout + (int64_t)first * p.ld_dout + (int64_t)h0 * p.d, p.ld_dout, queries, lg0,
-                  p.group, p.inv_group, p.d, p.narrow);
-    if (tid < RT) {
-      const int r = min(tid, cnt - 1), tg = div_group(lg0 + r, p.inv_group), head = h0 + lg0 + r - tg * p.group;
-      r_lse = p.lse[(int64_t)head * p.ld_lse + first + tg];
-      r_delta = p.delta[(int64_t)head * p.sum_q + first + tg];
-      r_pos = tid < cnt ? off + lt0 + tg : INT32_MIN;           // no key sees a row past the end
-    }
-    left_rows -= RT;
-    lt0 += step_t;
-    lg0 += step_g;
-    if (lg0 >= p.group) {
-      lg0 -= p.group;
-      ++lt0;
-    }
+  int t0 = ta, g0 = 0;
+  auto load = [&](int tile) {
+    in.load(p, tid, hk, q0, t0, g0, min(tb - t0, RT + 1), (int)min((int64_t)RT, rows - (int64_t)tile * RT), off);
   };
-  auto store = [&](int buf) {
-    sq.store(tid, Qb[buf]);
-    sg.store(tid, Gb[buf]);
-    if (tid < RT) {
-      lse_b[buf][tid] = r_lse == -INFINITY ? 0.f : r_lse * -kLog2e;   // -inf: a row that sees nothing
-      delta_b[buf][tid] = -r_delta;
-      pos_b[buf][tid] = r_pos;
-    }
-  };
-  int nt0 = ta, ng0 = 0;                                        // the tile that is worked on next
-  if (tiles > 0) {
-    load();
-    store(0);
-  }
+  if (tiles > 0) load(0);
   for (int tile = 0; tile < tiles; ++tile) {
     __syncthreads();
-    const T *Qs = Qb[tile & 1], *Gs = Gb[tile & 1];
-    const float *lse_s = lse_b[tile & 1], *delta_s = delta_b[tile & 1];
-    const int* pos_s = pos_b[tile & 1];
-    const int cur_rows = (int)min((int64_t)RT, rb - ra - (int64_t)tile * RT);
-    const int pa = off + nt0, pe = off + nt0 + (ng0 + cur_rows - 1) / p.group;
-    nt0 = lt0;
-    ng0 = lg0;
-    if (tile + 1 < tiles) load();
-    if (live && pe >= plo_a && pa <= phi_b) {
-    const bool whole = cur_rows == RT && pa >= plo_b && pe <= phi_a;
-    // One 32-row block after the other; each step issues the reads of the next
-    // one before its products, and the exponentials and score gradients run
-    // under products.  A hidden pair's score starts from -inf, so its weight is 0;
-    // dP starts from -D.
-    frag A[NS], B[NS], X[ND], Y[ND];
-    read_along<DP>(Qs, 0, lane, A);
-#pragma unroll
-    for (int rbk = 0; rbk < RB; ++rbk) {
-      const int r0 = 32 * rbk;
-      f32x16 S = f32x16{}, dP;
-      if (!whole) {
-#pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4) {
-          const int4 ps = *reinterpret_cast<const int4*>(pos_s + r0 + 8 * e4 + 4 * h32);
-          const int pr[4] = {ps.x, ps.y, ps.z, ps.w};
-#pragma unroll
-          for (int u = 0; u < 4; ++u) S[4 * e4 + u] = pr[u] >= plo && pr[u] <= phi ? 0.f : -INFINITY;
-        }
-      }
-      pin();
-      read_along<DP>(Gs, r0, lane, B);
-#pragma unroll
-      for (int e4 = 0; e4 < 4; ++e4) {
-        const f32x4 de = *reinterpret_cast<const f32x4*>(delta_s + r0 + 8 * e4 + 4 * h32);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) dP[4 * e4 + u] = de[u];
-      }
-      pin();
-      S = product(A, K, S);
-      pin();
-      read_across<DP>(Gs, r0, lane, tr, X);
-      pin();
-      dP = product(B, V, dP);
-      frag W, D;
-#pragma unroll
-      for (int e4 = 0; e4 < 4; ++e4) {
-        const f32x4 ls = *reinterpret_cast<const f32x4*>(lse_s + r0 + 8 * e4 + 4 * h32);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) S[4 * e4 + u] = __builtin_amdgcn_exp2f(fmaf(S[4 * e4 + u], p.c, ls[u]));
-      }
-      to_operand(S, 0, W);
-      pin();
-      read_across<DP>(Gs, r0 + 16, lane, tr, Y);
-      pin();
-      add_products(X, W, dV);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) dP[e] *= S[e];
-      to_operand(S, 1, W);
-      pin();
-      read_across<DP>(Qs, r0, lane, tr, X);
-      pin();
-      add_products(Y, W, dV);
-      to_operand(dP, 0, D);
-      pin();
-      read_across<DP>(Qs, r0 + 16, lane, tr, Y);
-      pin();
-      add_products(X, D, dK);
-      to_operand(dP, 1, D);
-      pin();
-      if (rbk + 1 < RB) read_along<DP>(Qs, r0 + 32, lane, A);
-      pin();
-      add_products(Y, D, dK);
+    in.store(tid, Qs, Gs, lse_s, delta_s, pos_s);
+    __syncthreads();
+    const int cnt = (int)min((int64_t)RT, rows - (int64_t)tile * RT);
+    const int pa = off + t0, pe = off + t0 + (g0 + cnt - 1) / p.group;
+    t0 += step_t;
+    g0 += step_g;
+    if (g0 >= p.group) {
+      g0 -= p.group;
+      ++t0;
     }
-    }
-    if (tile + 1 < tiles) store(~tile & 1);
+    if (tile + 1 < tiles) load(tile + 1);
+    if (!live || pe < plo_a || pa > phi_b) continue;       // no row of the tile sees a key of the wave
+    const bool whole = pa >= plo_b && pe <= phi_a;
+#pragma unroll
+    for (int r0 = 0; r0 < RT; r0 += 32)
+      key_block<T, DP>(Qs, Gs, lse_s, delta_s, pos_s, r0, whole, plo, phi, p.c, K, V, dK, dV, lane, tr);
   }
   if (!mine) return;
-  if (p.split && j < p.sinks && max(ta, tb) < n) {         // what the queries past the window add to a sink
-    const float* sum = p.sink_sum + (((int64_t)(i * p.kv_heads + hk) * p.subs + (j >> 5)) * 64 + (j & 31)) * DP;
-#pragma unroll
-    for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-      for (int e = 0; e < 16; e += 4) {
-        const int at = 32 * dt + 2 * e + 4 * h32;
-        const f32x4 a = *reinterpret_cast<const f32x4*>(sum + at), w = *reinterpret_cast<const f32x4*>(sum + 32 * DP + at);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          dK[dt][e + u] += a[u];
-          dV[dt][e + u] += w[u];
-        }
-      }
-  }
-  T* kd = (T*)p.dk + (int64_t)(k0 + j) * p.ld_dk + (int64_t)hk * p.d;
-  T* vd = (T*)p.dv + (int64_t)(k0 + j) * p.ld_dv + (int64_t)hk * p.d;
+  const bool more = p.split && j < p.sinks && tb < n;      // what the queries past the window add to a sink
+  const float* sum = p.sink_sum + (((int64_t)(i * p.kv_heads + hk) * p.subs + (j >> 5)) * 64 + (j & 31)) * DP;
 #pragma unroll
   for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
     for (int e = 0; e < 16; e += 4) {
       const int at = 32 * dt + 2 * e + 4 * h32;
-      if (at < p.d) {
-        typedef T vec4 __attribute__((ext_vector_type(4)));
-        vec4 a, w;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          a[u] = (T)(dK[dt][e + u] * p.scale);
-          w[u] = (T)dV[dt][e + u];
-        }
-        *reinterpret_cast<vec4*>(kd + at) = a;
-        *reinterpret_cast<vec4*>(vd + at) = w;
+      if (at >= p.d) continue;
+      f32x4 a = {dK[dt][e], dK[dt][e + 1], dK[dt][e + 2], dK[dt][e + 3]};
+      f32x4 w = {dV[dt][e], dV[dt][e + 1], dV[dt][e + 2], dV[dt][e + 3]};
+      if (more) {
+        a += *reinterpret_cast<const f32x4*>(sum + at);
+        w += *reinterpret_cast<const f32x4*>(sum + 32 * DP + at);
       }
+      write_keys<T>(p, k0 + j, hk, at, a, w);
     }
 }
 
-// The sinks' gradients from the queries past their window: few keys and all the
-// later rows of the sample, which one workgroup per block of keys would walk
-// alone while the others have left.  A workgroup takes 32 sinks and a piece of
-// the rows, 32 rows of each tile of 128 per wave; every row sees every sink here,
-// so there is no mask.  The waves' sums are added in order through LDS, the
-// pieces' by sink_sum_kernel.
-template <typename T, int DP>
-__global__ void __launch_bounds__(256)
-window_sink_kernel(WindowBwdParams p) {
+// dK and dV of 32 keys per workgroup, its four waves on different tiles of rows,
+// each with its own tile in LDS, their sums joined in order at the end.  Two uses:
+// - calls whose blocks of 128 keys would leave most of the card idle;
+// - SINKS: the sinks' gradients from the queries past their window, few keys and
+//   all the later rows of the sample, which the workgroup of a block of keys would
+//   walk alone while the others have left.  A workgroup takes a piece of the rows
+//   (every row sees every sink there) and leaves its sums for sink_sum_kernel.
+template <typename T, int DP, bool SINKS>
+__global__ void __launch_bounds__(256, sizeof(T) == 4 || DP == 128 ? 1 : 2)
+window_dkv_few_kernel(WindowBwdParams p) {
   typedef typename Frag<T>::type frag;
-  constexpr int RT = 128, NS = DP / 16, ND = DP / 32;
+  constexpr int RT = 32, ND = DP / 32, kOutLd = DP + 4;
+  struct Rows {
+    T q[RT * Tile<T, DP>::kLd], g[RT * Tile<T, DP>::kLd];
+    float lse[RT], delta[RT];
+    int pos[RT];
+  };
   union Shared {
-    struct {
-      T q[RT * Tile<T, DP>::kLd], g[RT * Tile<T, DP>::kLd];
-      float lse[RT], delta[RT];
-    } t;
-    float sum[4][32 * DP];
+    Rows tile[4];
+    float sum[4][32 * kOutLd];
   };
   __shared__ __attribute__((aligned(16))) Shared sh;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h32 = lane >> 5;
   const int64_t item = block_id();
   if (item >= p.items) return;
-  const int hk = (int)(item % p.kv_heads), piece = (int)(item / p.kv_heads % p.pieces);
-  const int sub = (int)(item / p.kv_heads / p.pieces % p.subs), i = (int)(item / p.kv_heads / p.pieces / p.subs);
-  const int q0 = p.cu_q[i], n = p.cu_q[i + 1] - q0, k0 = p.cu_k[i], m = p.cu_k[i + 1] - k0, off = m - n;
-  const int sinks = min(p.sinks, m);
-  if (sub * 32 >= sinks) return;
-  const int jb = sub * 32 & ~127, jl = min(jb + 127, m - 1);
-  const int ta = p.right >= 0 ? min(max(0, jb - p.right - off), n) : 0;
-  const int64_t ra = (int64_t)max(ta, window_end(jl, p.left, off, n)) * p.group + (int64_t)piece * p.piece;
-  const int64_t rb = min((int64_t)n * p.group, ra + p.piece);
-  if (ra >= rb) return;
-  const int j = min(sub * 32 + (lane & 31), sinks - 1);
-  frag K[NS], V[NS];
-  {
-    const T* ksrc = (const T*)p.k + (int64_t)(k0 + j) * p.ld_k + (int64_t)hk * p.d;
-    const T* vsrc = (const T*)p.v + (int64_t)(k0 + j) * p.ld_v + (int64_t)hk * p.d;
-#pragma unroll
-    for (int ks = 0; ks < NS; ++ks) {
-      const int e = 16 * ks + 8 * h32;
-      frag z = {};
-      K[ks] = e < p.d ? *reinterpret_cast<const frag*>(ksrc + e) : z;
-      V[ks] = e < p.d ? *reinterpret_cast<const frag*>(vsrc + e) : z;
-    }
-    multiply<T>(K, p.qmul);
+  const int hk = (int)(item % p.kv_heads);
+  int i, sub = 0, piece = 0, jb;
+  if (SINKS) {
+    piece = (int)(item / p.kv_heads % p.pieces);
+    sub = (int)(item / p.kv_heads / p.pieces % p.subs);
+    i = (int)(item / p.kv_heads / p.pieces / p.subs);
+    jb = 32 * sub;
+  } else {
+    const int64_t b = item / p.kv_heads;
+    i = find_sample(p.cu_k, p.batch, 1, kFewShift, b, lane);
+    jb = (int)((b - block_start(p.cu_k, i, 1, kFewShift)) << kFewShift);
   }
+  const int q0 = p.cu_q[i], n = p.cu_q[i + 1] - q0, k0 = p.cu_k[i], m = p.cu_k[i + 1] - k0, off = m - n;
+  const int keys = SINKS ? min(p.sinks, m) : m;            // the keys that matter here
+  if (jb >= keys) return;
+  const int je = min(jb + 31, keys - 1), j = min(jb + (lane & 31), keys - 1);
+  const int plo = first_seeing(p, j), phi = last_seeing(p, j);
+  const int plo_b = first_seeing(p, je), phi_a = last_seeing_all(p, jb, je);
+  // the rows: with a window up to its end, where the sinks' own call begins
+  const int blk_end = min((jb & ~127) + 127, m - 1);       // last key of the block of 128, which sets that end
+  const int ta = p.right >= 0 ? min(max(0, (SINKS ? jb & ~127 : jb) - p.right - off), n) : 0;
+  const int far = p.left >= 0 ? max(ta, window_end(blk_end, p.left, off, n)) : n;
+  int64_t ra, rb;
+  if (SINKS) {
+    ra = (int64_t)far * p.group + (int64_t)piece * p.piece;
+    rb = min((int64_t)n * p.group, ra + p.piece);
+  } else {
+    ra = (int64_t)ta * p.group;
+    rb = (int64_t)(jb >= p.sinks ? min(far, max(ta, window_end(je, p.left >= 0 ? p.left : n + m, off, n)))
+                   : p.split ? far : n) * p.group;
+  }
+  if (SINKS && ra >= rb) return;
+  frag K[DP / 16], V[DP / 16];
+  load_keys<T, DP>(p, k0 + j, hk, h32, K, V);
   uint32_t tr[2];
   Tile<T, DP>::across_addr(lane, tr);
   f32x16 dK[ND], dV[ND];
 #pragma unroll
   for (int dt = 0; dt < ND; ++dt) dK[dt] = dV[dt] = f32x16{};
-  Stage<T, DP, RT, 256> sq, sg;
-  for (int64_t r0 = ra; r0 < rb; r0 += RT) {
-    const int t0 = (int)(r0 / p.group), g0 = (int)(r0 - (int64_t)t0 * p.group);
-    const int cnt = (int)min((int64_t)RT, rb - r0), first = q0 + t0, h0 = hk * p.group;
-    const int queries = min(n - t0, RT + 1);
-    sq.load_group(tid, (const T*)p.q + (int64_t)first * p.ld_q + (int64_t)h0 * p.d, p.ld_q, queries, g0, p.group,
-                  p.inv_group, p.d, p.narrow);
-    sg.load_group(tid, (const T*)p.dout + (int64_t)first * p.ld_dout + (int64_t)h0 * p.d, p.ld_dout, queries, g0, p.group,
-                  p.inv_group, p.d, p.narrow);
-    float lse2 = INFINITY, delta = 0.f;                    // a row past the piece has weight 0
-    if (tid < cnt) {
-      const int tg = div_group(g0 + tid, p.inv_group), head = h0 + g0 + tid - tg * p.group;
-      lse2 = p.lse[(int64_t)head * p.ld_lse + first + tg] * kLog2e;
-      delta = p.delta[(int64_t)head * p.sum_q + first + tg];
+  RowTile<T, DP, RT, 64> in;
+  Rows& my = sh.tile[wave];
+  const int64_t first = ra + RT * wave;
+  int t0 = (int)(first / p.group), g0 = (int)(first - (int64_t)t0 * p.group);
+  const int step_t = 4 * RT / p.group, step_g = 4 * RT - step_t * p.group;
+  const int t_end = (int)((rb + p.group - 1) / p.group);
+  auto load = [&](int64_t r) {
+    in.load(p, lane, hk, q0, t0, g0, min(t_end - t0, RT + 1), (int)min((int64_t)RT, rb - r), off);
+  };
+  auto own = [] {                                          // the tile is the wave's own
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+  if (first < rb) load(first);
+  for (int64_t r = first; r < rb; r += 4 * RT) {
+    own();
+    in.store(lane, my.q, my.g, my.lse, my.delta, my.pos);
+    own();
+    const int pa = off + t0, pe = off + t0 + (g0 + (int)min((int64_t)RT, rb - r) - 1) / p.group;
+    t0 += step_t;
+    g0 += step_g;
+    if (g0 >= p.group) {
+      g0 -= p.group;
+      ++t0;
     }
-    __syncthreads();
-    sq.store(tid, sh.t.q);
-    sg.store(tid, sh.t.g);
-    if (tid < RT) {
-      sh.t.lse[tid] = lse2;
-      sh.t.delta[tid] = delta;
-    }
-    __syncthreads();
-    const int rw = 32 * wave;
-    if (rw >= cnt) continue;
-    f32x16 S = f32x16{}, dP = f32x16{};
-#pragma unroll
-    for (int ks = 0; ks < NS; ++ks) {
-      S = mma32(Tile<T, DP>::along(sh.t.q, rw, ks, lane), K[ks], S);
-      dP = mma32(Tile<T, DP>::along(sh.t.g, rw, ks, lane), V[ks], dP);
-    }
-#pragma unroll
-    for (int e4 = 0; e4 < 4; ++e4) {
-      const int r = rw + 8 * e4 + 4 * h32;
-      const f32x4 ls = *reinterpret_cast<const f32x4*>(sh.t.lse + r), de = *reinterpret_cast<const f32x4*>(sh.t.delta + r);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const float w = __builtin_amdgcn_exp2f(fmaf(S[4 * e4 + u], p.c, -ls[u]));
-        S[4 * e4 + u] = w;
-        dP[4 * e4 + u] = w * (dP[4 * e4 + u] - de[u]);
-      }
-    }
-#pragma unroll
-    for (int nn = 0; nn < 2; ++nn) {
-      frag W, D;
-      to_operand(S, nn, W);
-      to_operand(dP, nn, D);
-#pragma unroll
-      for (int dt = 0; dt < ND; ++dt) {
-        dV[dt] = mma32(across<DP>(sh.t.g, rw + 16 * nn, dt, lane, tr), W, dV[dt]);
-        dK[dt] = mma32(across<DP>(sh.t.q, rw + 16 * nn, dt, lane, tr), D, dK[dt]);
-      }
-    }
+    if (r + 4 * RT < rb) load(r + 4 * RT);
+    key_block<T, DP>(my.q, my.g, my.lse, my.delta, my.pos, 0, SINKS || (pa >= plo_b && pe <= phi_a), plo, phi, p.c, K, V,
+                     dK, dV, lane, tr);
   }
-  float* out = p.sink_part + ((((int64_t)i * p.kv_heads + hk) * p.subs + sub) * p.pieces + piece) * 64 * DP;
+  // the four waves' sums: dK, then dV, four channels per thread and turn
+  constexpr int kTurns = 32 * DP / 4 / 256 > 0 ? 32 * DP / 4 / 256 : 1;
+  f32x4 total[2][kTurns];
 #pragma unroll
-  for (int x = 0; x < 2; ++x) {                            // dK, then dV
+  for (int x = 0; x < 2; ++x) {
     __syncthreads();
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
       for (int e = 0; e < 16; e += 4) {
         const f32x16& a = x ? dV[dt] : dK[dt];
-        *reinterpret_cast<f32x4*>(&sh.sum[wave][(lane & 31) * DP + 32 * dt + 2 * e + 4 * h32]) =
+        *reinterpret_cast<f32x4*>(&sh.sum[wave][(lane & 31) * kOutLd + 32 * dt + 2 * e + 4 * h32]) =
             f32x4{a[e], a[e + 1], a[e + 2], a[e + 3]};
       }
     __syncthreads();
-    for (int u = tid * 4; u < 32 * DP; u += 1024) {
-      f32x4 a = *reinterpret_cast<f32x4*>(&sh.sum[0][u]);
 #pragma unroll
-      for (int w = 1; w < 4; ++w) a += *reinterpret_cast<f32x4*>(&sh.sum[w][u]);
-      *reinterpret_cast<f32x4*>(out + x * 32 * DP + u) = a;
+    for (int u = 0; u < kTurns; ++u) {
+      const int y = tid + 256 * u, at = y / (DP / 4) * kOutLd + y % (DP / 4) * 4;
+      total[x][u] = *reinterpret_cast<f32x4*>(&sh.sum[0][at]);
+#pragma unroll
+      for (int w = 1; w < 4; ++w) total[x][u] += *reinterpret_cast<f32x4*>(&sh.sum[w][at]);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kTurns; ++u) {
+    const int y = tid + 256 * u, key = y / (DP / 4), at = y % (DP / 4) * 4;
+    if (SINKS) {
+      float* out = p.sink_part + ((((int64_t)i * p.kv_heads + hk) * p.subs + sub) * p.pieces + piece) * 64 * DP;
+      *reinterpret_cast<f32x4*>(out + key * DP + at) = total[0][u];
+      *reinterpret_cast<f32x4*>(out + (32 + key) * DP + at) = total[1][u];
+    } else if (jb + key < m && at < p.d) {
+      if (p.split && jb + key < p.sinks && far < n) {
+        const float* sum = p.sink_sum + (((int64_t)(i * p.kv_heads + hk) * p.subs + (jb >> 5)) * 64 + key) * DP + at;
+        total[0][u] += *reinterpret_cast<const f32x4*>(sum);
+        total[1][u] += *reinterpret_cast<const f32x4*>(sum + 32 * DP);
+      }
+      write_keys<T>(p, k0 + jb + key, hk, at, total[0][u], total[1][u]);
     }
   }
 }
@@ -578,20 +752,36 @@ SinkPlan sink_plan(const nt_window_args& a) {
 }
 
 template <typename T, int DP>
-hipError_t launch_backward(WindowBwdParams p, int64_t q_items, int64_t k_items, hipStream_t s) {
-  p.items = q_items;
-  if (q_items > 0) window_dq_kernel<T, DP><<<folded_grid(q_items), 256, 0, s>>>(p);
+hipError_t launch_backward(WindowBwdParams p, const nt_layout& Lq, const nt_layout& Lk, hipStream_t s) {
+  // blocks of 128 rows or keys, or of 32 where those would leave most of the card idle
+  auto blocks = [&](const nt_layout& L, int mul) {
+    int64_t n = 0;
+    for (int32_t x : L.lengths) n += ((int64_t)x * mul + 127) >> 7;
+    return n * p.kv_heads;
+  };
+  auto items = [&](const nt_layout& L, int mul, int shift) {
+    return L.sum_n ? block_count(L.sum_n, L.batch, mul, shift) * p.kv_heads : 0;
+  };
+  const bool few_q = blocks(Lq, p.group) <= kFewRowBlocks, few_k = blocks(Lk, 1) <= kFewKeyBlocks;
+  p.items = items(Lq, p.group, few_q ? kFewShift : kBlockShift);
+  if (p.items > 0) {
+    if (few_q) window_dq_few_kernel<T, DP><<<folded_grid(p.items), 256, 0, s>>>(p);
+    else window_dq_kernel<T, DP><<<folded_grid(p.items), 256, 0, s>>>(p);
+  }
   if (hipError_t e = hipGetLastError()) return e;
   if (p.split) {
     p.items = (int64_t)p.batch * p.kv_heads * p.subs * p.pieces;
-    window_sink_kernel<T, DP><<<folded_grid(p.items), 256, 0, s>>>(p);
+    window_dkv_few_kernel<T, DP, true><<<folded_grid(p.items), 256, 0, s>>>(p);
     if (hipError_t e = hipGetLastError()) return e;
     p.items = (int64_t)p.batch * p.kv_heads * p.subs * (64 * DP / 1024);
     sink_sum_kernel<DP><<<folded_grid(p.items), 256, 0, s>>>(p);
     if (hipError_t e = hipGetLastError()) return e;
   }
-  p.items = k_items;
-  if (k_items > 0) window_dkv_kernel<T, DP><<<folded_grid(k_items), 256, 0, s>>>(p);
+  p.items = items(Lk, 1, few_k ? kFewShift : kBlockShift);
+  if (p.items > 0) {
+    if (few_k) window_dkv_few_kernel<T, DP, false><<<folded_grid(p.items), 256, 0, s>>>(p);
+    else window_dkv_kernel<T, DP><<<folded_grid(p.items), 256, 0, s>>>(p);
+  }
   return hipGetLastError();
 }
 
@@ -633,15 +823,13 @@ hipError_t launch_window_backward(const nt_window_args& a, hipStream_t s) {
   p.piece = sp.piece;
   p.sink_part = (float*)((char*)a.workspace + sp.delta_bytes);
   p.sink_sum = (float*)((char*)a.workspace + sp.delta_bytes + sp.part_bytes);
-  const int64_t qi = Lq.sum_n ? win::block_count(Lq.sum_n, Lq.batch, p.group, kBlockShift) * p.kv_heads : 0;
-  const int64_t ki = Lk.sum_n ? win::block_count(Lk.sum_n, Lk.batch, 1, kBlockShift) * p.kv_heads : 0;
   const bool bf = a.dtype == NT_BF16;
   const int size = bf ? 2 : 4;
   p.narrow = win::narrow_stride(a.ld_q, size) && win::narrow_stride(a.ld_dout, size) &&
              win::narrow_stride(a.ld_k, size) && win::narrow_stride(a.ld_v, size);
-  if (p.d <= 32) return bf ? launch_backward<bf16, 32>(p, qi, ki, s) : launch_backward<float, 32>(p, qi, ki, s);
-  if (p.d <= 64) return bf ? launch_backward<bf16, 64>(p, qi, ki, s) : launch_backward<float, 64>(p, qi, ki, s);
-  return bf ? launch_backward<bf16, 128>(p, qi, ki, s) : launch_backward<float, 128>(p, qi, ki, s);
+  if (p.d <= 32) return bf ? launch_backward<bf16, 32>(p, Lq, Lk, s) : launch_backward<float, 32>(p, Lq, Lk, s);
+  if (p.d <= 64) return bf ? launch_backward<bf16, 64>(p, Lq, Lk, s) : launch_backward<float, 64>(p, Lq, Lk, s);
+  return bf ? launch_backward<bf16, 128>(p, Lq, Lk, s) : launch_backward<float, 128>(p, Lq, Lk, s);
 }
 
 }  // namespace nt

@@ -223,10 +223,22 @@ __device__ __forceinline__ void read_along(const T* s, int base, int lane, F (&o
 #pragma unroll
   for (int ks = 0; ks < DP / 16; ++ks) out[ks] = Tile<T, DP>::along(s, base, ks, lane);
 }
-template <int DP, typename T, typename F>
-__device__ __forceinline__ void read_across(const T* s, int base, int lane, const uint32_t (&tr)[2], F (&out)[DP / 32]) {
+template <int DP, typename T, typename F, int M>
+__device__ __forceinline__ void read_across(const T* s, int base, int lane, const uint32_t (&tr)[2], F (&out)[M]) {
 #pragma unroll
   for (int dt = 0; dt < DP / 32; ++dt) out[dt] = across<DP>(s, base, dt, lane, tr);
+}
+// fragments ks0 .. ks0 + N - 1 of a row block
+template <int DP, int N, typename T, typename F, int M>
+__device__ __forceinline__ void read_part(const T* s, int base, int ks0, int lane, F (&out)[M]) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) out[k] = Tile<T, DP>::along(s, base, ks0 + k, lane);
+}
+template <int N, typename F>
+__device__ __forceinline__ f32x16 product_part(const F* a, const F* b, f32x16 s) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) s = mma32(a[k], b[k], s);
+  return s;
 }
 template <int N, typename F>
 __device__ __forceinline__ f32x16 product(const F (&a)[N], const F (&b)[N], f32x16 s = f32x16{}) {
@@ -234,8 +246,8 @@ __device__ __forceinline__ f32x16 product(const F (&a)[N], const F (&b)[N], f32x
   for (int k = 0; k < N; ++k) s = mma32(a[k], b[k], s);
   return s;
 }
-template <int N, typename F>
-__device__ __forceinline__ void add_products(const F (&a)[N], const F& b, f32x16 (&acc)[N]) {
+template <int N, typename F, int M>
+__device__ __forceinline__ void add_products(const F (&a)[M], const F& b, f32x16 (&acc)[N]) {
 #pragma unroll
   for (int k = 0; k < N; ++k) acc[k] = mma32(a[k], b, acc[k]);
 }
