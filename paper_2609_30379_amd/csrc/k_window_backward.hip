@@ -308,8 +308,8 @@ window_dq_few_kernel(WindowBwdParams p) {
 
 // One block of 32 rows (in LDS from row r0) against the wave's 32 keys, in steps of
 // at most four fragments: each step issues the reads of the next one before its
-// products, and the exponentials and score gradients run under products.  lse_s
-// holds -lse log2(e) (-inf for a row past the end: weight 0), delta_s -D, pos_s the
+// products, and the exponentials and score gradients run under products (the
+// compiler keeps to that order by itself here).  lse_s holds -lse log2(e) (-inf for a row past the end: weight 0), delta_s -D, pos_s the
 // rows' positions; a hidden pair's score starts from -inf.
 template <typename T, int DP>
 __device__ __forceinline__ void key_block(const T* Qs, const T* Gs, const float* lse_s, const float* delta_s,
@@ -332,22 +332,15 @@ __device__ __forceinline__ void key_block(const T* Qs, const T* Gs, const float*
       for (int u = 0; u < 4; ++u) S[4 * e4 + u] = pr[u] >= plo && pr[u] <= phi ? 0.f : -INFINITY;
     }
   }
-  pin();
   if constexpr (NS > kG) {
     read_part<DP, kG>(Qs, r0, kG, lane, Y);
-    pin();
-    S = product_part<kG>(X, K, S);
-    pin();
-    read_part<DP, kG>(Gs, r0, 0, lane, X);
-    pin();
-    S = product_part<kG>(Y, K + kG, S);
-    pin();
-  } else {
+      S = product_part<kG>(X, K, S);
+      read_part<DP, kG>(Gs, r0, 0, lane, X);
+      S = product_part<kG>(Y, K + kG, S);
+    } else {
     read_part<DP, kG>(Gs, r0, 0, lane, Y);
-    pin();
-    S = product_part<kG>(X, K, S);
-    pin();
-#pragma unroll
+      S = product_part<kG>(X, K, S);
+  #pragma unroll
     for (int k = 0; k < kG; ++k) X[k] = Y[k];
   }
 #pragma unroll
@@ -358,16 +351,12 @@ __device__ __forceinline__ void key_block(const T* Qs, const T* Gs, const float*
   }
   if constexpr (NS > kG) {
     read_part<DP, kG>(Gs, r0, kG, lane, Y);
-    pin();
-    dP = product_part<kG>(X, V, dP);
-    pin();
-    read_across<DP>(Gs, r0, lane, tr, X);
-    pin();
-    dP = product_part<kG>(Y, V + kG, dP);
+      dP = product_part<kG>(X, V, dP);
+      read_across<DP>(Gs, r0, lane, tr, X);
+      dP = product_part<kG>(Y, V + kG, dP);
   } else {
     read_across<DP>(Gs, r0, lane, tr, Y);
-    pin();
-    dP = product_part<kG>(X, V, dP);
+      dP = product_part<kG>(X, V, dP);
 #pragma unroll
     for (int k = 0; k < ND; ++k) X[k] = Y[k];
   }
@@ -378,24 +367,17 @@ __device__ __forceinline__ void key_block(const T* Qs, const T* Gs, const float*
     for (int u = 0; u < 4; ++u) S[4 * e4 + u] = __builtin_amdgcn_exp2f(fmaf(S[4 * e4 + u], c, ls[u]));
   }
   to_operand(S, 0, W);
-  pin();
   read_across<DP>(Gs, r0 + 16, lane, tr, Y);
-  pin();
   add_products(X, W, dV);
 #pragma unroll
   for (int e = 0; e < 16; ++e) dP[e] *= S[e];
   to_operand(S, 1, W);
-  pin();
   read_across<DP>(Qs, r0, lane, tr, X);
-  pin();
   add_products(Y, W, dV);
   to_operand(dP, 0, W);
-  pin();
   read_across<DP>(Qs, r0 + 16, lane, tr, Y);
-  pin();
   add_products(X, W, dK);
   to_operand(dP, 1, W);
-  pin();
   add_products(Y, W, dK);
 }
 
@@ -446,8 +428,9 @@ __device__ __forceinline__ void write_keys(const WindowBwdParams& p, int64_t row
 // share the keys, and the rows' statistics.  THREADS threads of index tid.
 template <typename T, int DP, int RT, int THREADS> struct RowTile {
   Stage<T, DP, RT, THREADS> q, g;
-  float lse, delta;
+  float lse, delta;              // as loaded: touching them here would wait for all loads of the tile
   int pos;
+  bool inside;
   // cnt rows from row g0 of query t0 of the sample that begins at q0
   __device__ __forceinline__ void load(const WindowBwdParams& p, int tid, int hk, int q0, int t0, int g0, int queries,
                                        int cnt, int off) {
@@ -461,14 +444,15 @@ template <typename T, int DP, int RT, int THREADS> struct RowTile {
       lse = p.lse[(int64_t)head * p.ld_lse + first + tg];
       delta = p.delta[(int64_t)head * p.sum_q + first + tg];
       pos = off + t0 + tg;
-      if (tid >= cnt) lse = INFINITY;
+      inside = tid < cnt;
     }
   }
   __device__ __forceinline__ void store(int tid, T* qs, T* gs, float* lse_s, float* delta_s, int* pos_s) const {
     q.store(tid, qs);
     g.store(tid, gs);
     if (tid < RT) {
-      lse_s[tid] = lse == -INFINITY ? 0.f : lse * -kLog2e;   // -inf: a row that sees nothing, hidden everywhere
+      // a row past the end has weight 0; one that sees nothing (-inf) is hidden everywhere
+      lse_s[tid] = !inside ? -INFINITY : lse == -INFINITY ? 0.f : lse * -kLog2e;
       delta_s[tid] = -delta;
       pos_s[tid] = pos;
     }
@@ -538,7 +522,7 @@ window_dkv_kernel(WindowBwdParams p) {
     if (tile + 1 < tiles) load(tile + 1);
     if (!live || pe < plo_a || pa > phi_b) continue;       // no row of the tile sees a key of the wave
     const bool whole = pa >= plo_b && pe <= phi_a;
-#pragma unroll
+#pragma unroll 1
     for (int r0 = 0; r0 < RT; r0 += 32)
       key_block<T, DP>(Qs, Gs, lse_s, delta_s, pos_s, r0, whole, plo, phi, p.c, K, V, dK, dV, lane, tr);
   }

@@ -159,7 +159,7 @@ template <typename T, int DP, int ROWS, int THREADS> struct Stage {
     const int r0 = tid / kP, c = tid % kP;
     if (narrow) {
       const auto rs = buffer(base, ((int64_t)(rows - 1) * ld + d) * (int)sizeof(T));
-      const uint32_t ldb = (uint32_t)ld * sizeof(T), at = c * kE < d ? r0 * ldb + c * 16 : kOutside;
+      const uint32_t ldb = (uint32_t)ld * sizeof(T), at = r0 * ldb + c * 16 + (c * kE < d ? 0 : kOutside);
 #pragma unroll
       for (int i = 0; i < kPer; ++i)
         v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, at + i * (kStep * ldb), 0, 0));
@@ -179,11 +179,11 @@ template <typename T, int DP, int ROWS, int THREADS> struct Stage {
     const int r0 = tid / kP, c = tid % kP;
     if (narrow) {
       const auto rs = buffer(base, ((int64_t)(queries - 1) * ld + (int64_t)group * d) * (int)sizeof(T));
-      const uint32_t ldb = (uint32_t)ld * sizeof(T), db = (uint32_t)d * sizeof(T);
+      const uint32_t ldb = (uint32_t)ld * sizeof(T), db = (uint32_t)d * sizeof(T), c16 = c * 16 + (c * kE < d ? 0 : kOutside);
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
         const int x = g0 + r0 + i * kStep, tg = div_group(x, inv_group);
-        const uint32_t at = c * kE < d ? tg * ldb + (x - tg * group) * db + c * 16 : kOutside;
+        const uint32_t at = tg * ldb + (x - tg * group) * db + c16;
         v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, at, 0, 0));
       }
     } else {
