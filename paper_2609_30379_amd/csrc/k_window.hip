@@ -44,16 +44,11 @@ constexpr int kFewChunk = 32, kRowsChunk = 8, kSplitItems = 512;
 // One tile of KB x 32 keys against the wave's 32 rows: scores S become weights, O
 // and l are brought to the maximum in use.
 template <int KB, int ND>
-__device__ __forceinline__ void online_softmax(f32x16 (&S)[KB], f32x16 (&O)[ND], float& mx, float& l, float c, bool whole,
-                                               int j0, int jend, int lo, int hi, int sinks, int h32) {
-  if (!whole)
+__device__ __forceinline__ void online_softmax(f32x16 (&S)[KB], f32x16 (&O)[ND], float& mx, float& l, float c,
+                                               const TileMask& mask) {
+  if (mask.cut_hi || mask.cut_lo)
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int j = j0 + 32 * kb + 8 * (e >> 2) + 4 * h32 + (e & 3);
-        S[kb][e] = j < jend && j <= hi && (j >= lo || j < sinks) ? S[kb][e] : -INFINITY;
-      }
+    for (int kb = 0; kb < KB; ++kb) mask.hide(S[kb], kb);
   float top = S[0][0];
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb)
@@ -158,27 +153,28 @@ window_rows_kernel(WindowParams p) {
   // The next tile's keys travel while the scores of this one are computed, its
   // values while the weights are applied: one set of registers for both.
   Stage<T, DP, KT, 256> stage;
-  auto load = [&](const T* base, int64_t ld, int tile) {
+  auto load = [&](auto& to, const T* base, int64_t ld, int tile) {
     const int j0 = kt.first(tile, KT), cnt = min(kt.end(tile) - j0, KT);
-    stage.load(tid, base + (int64_t)(k0 + j0) * ld, ld, cnt, p.d, p.narrow);
+    to.load(tid, base + (int64_t)(k0 + j0) * ld, ld, cnt, p.d, p.narrow);
   };
   const int first = split * p.chunk, end = min(kt.n, first + p.chunk);
   if (first < end) {
-    load(kbase, p.ld_k, first);
+    Stage<T, DP, KT, 256> values;                          // both in flight at once
+    load(stage, kbase, p.ld_k, first);
+    load(values, vbase, p.ld_v, first);
     stage.store(tid, Kb[0]);
-    load(vbase, p.ld_v, first);
-    stage.store(tid, Vb[0]);
+    values.store(tid, Vb[0]);
   }
   // one tile from buffer B while the next one is on its way into the other: a
   // constant, so that all LDS addresses of the loop are offsets of a few registers
   auto body = [&](auto B, int tile) {
     __syncthreads();
     const T *Ks = Kb[B.value], *Vs = Vb[B.value];
-    if (tile + 1 < end) load(kbase, p.ld_k, tile + 1);
+    if (tile + 1 < end) load(stage, kbase, p.ld_k, tile + 1);
     const int j0 = kt.first(tile, KT), jend = kt.end(tile);
     // unless nothing of the tile is visible to any row of the wave
     const bool seen = live && j0 <= hi_b && (min(j0 + KT, jend) > lo_a || j0 < p.sinks);
-    const bool whole = j0 + KT <= jend && j0 + KT - 1 <= hi_a && (j0 >= lo_b || j0 + KT <= p.sinks);
+    const TileMask mask(j0, KT, jend, lo, hi, hi_a, lo_b, p.sinks, h32);
     // steps of at most four fragments, the reads of a step before the products of
     // the one before
     f32x16 S[KB];
@@ -207,11 +203,11 @@ window_rows_kernel(WindowParams p) {
             for (int k = 0; k < kG; ++k) X[k] = Y[k];
         }
       }
-      online_softmax<KB, ND>(S, O, mx, l, p.c, whole, j0, jend, lo, hi, p.sinks, h32);
+      online_softmax<KB, ND>(S, O, mx, l, p.c, mask);
     }
     if (tile + 1 < end) {
       stage.store(tid, Kb[1 - B.value]);
-      load(vbase, p.ld_v, tile + 1);
+      load(stage, vbase, p.ld_v, tile + 1);
     }
     if (seen) {
       read_across<DP>(Vs, 0, lane, tr, X);
@@ -348,7 +344,7 @@ window_few_kernel(WindowParams p) {
     own();
     if (tile + 4 < end) load(tile + 4);
     const int j0 = kt.first(tile, KT), jend = kt.end(tile);
-    const bool whole = j0 + KT <= jend && j0 + KT - 1 <= hi_a && (j0 >= lo_b || j0 + KT <= p.sinks);
+    const TileMask mask(j0, KT, jend, lo, hi, hi_a, lo_b, p.sinks, h32);
     f32x16 S[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
@@ -356,7 +352,7 @@ window_few_kernel(WindowParams p) {
       read_along<DP>(Ks, 32 * kb, lane, A);
       S[kb] = product(A, Q);
     }
-    online_softmax<KB, ND>(S, O, mx, l, p.c, whole, j0, jend, lo, hi, p.sinks, h32);
+    online_softmax<KB, ND>(S, O, mx, l, p.c, mask);
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll

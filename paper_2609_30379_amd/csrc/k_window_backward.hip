@@ -121,23 +121,24 @@ window_dq_kernel(WindowBwdParams p) {
   // the next tile's keys travel during the first half of this one, its values
   // during the second: one set of registers for both
   Stage<T, DP, KT, 256> stage;
-  auto load = [&](const T* base, int64_t ld, int tile) {
+  auto load = [&](auto& to, const T* base, int64_t ld, int tile) {
     const int j0 = kt.first(tile, KT), cnt = min(kt.end(tile) - j0, KT);
-    stage.load(tid, base + (int64_t)(k0 + j0) * ld, ld, cnt, p.d, p.narrow);
+    to.load(tid, base + (int64_t)(k0 + j0) * ld, ld, cnt, p.d, p.narrow);
   };
   if (kt.n > 0) {
-    load(kbase, p.ld_k, 0);
+    Stage<T, DP, KT, 256> values;                          // both in flight at once
+    load(stage, kbase, p.ld_k, 0);
+    load(values, vbase, p.ld_v, 0);
     stage.store(tid, Kb[0]);
-    load(vbase, p.ld_v, 0);
-    stage.store(tid, Vb[0]);
+    values.store(tid, Vb[0]);
   }
   auto body = [&](auto B, int tile) {                      // one tile from buffer B, a constant
     __syncthreads();
     const T *Ks = Kb[B.value], *Vs = Vb[B.value];
-    if (tile + 1 < kt.n) load(kbase, p.ld_k, tile + 1);
+    if (tile + 1 < kt.n) load(stage, kbase, p.ld_k, tile + 1);
     const int j0 = kt.first(tile, KT), jend = kt.end(tile);
     const bool seen = live && j0 <= hi_b && (min(j0 + KT, jend) > lo_a || j0 < p.sinks);
-    const bool whole = j0 + KT <= jend && j0 + KT - 1 <= hi_a && (j0 >= lo_b || j0 + KT <= p.sinks);
+    const TileMask mask(j0, KT, jend, lo, hi, hi_a, lo_b, p.sinks, h32);
     // Block by block of 32 keys in steps of at most four fragments, the reads of a
     // step before the products of the one before; a hidden pair's score starts
     // from -inf, dP from -D.
@@ -147,13 +148,7 @@ window_dq_kernel(WindowBwdParams p) {
       if (seen) {
       read_part<DP, kG>(Ks, 32 * kb, 0, lane, X);
       f32x16 S = f32x16{}, dP;
-      if (!whole) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int j = j0 + 32 * kb + 8 * (e >> 2) + 4 * h32 + (e & 3);
-          S[e] = j < jend && j <= hi && (j >= lo || j < p.sinks) ? 0.f : -INFINITY;
-        }
-      }
+      mask.hide(S, kb);
 #pragma unroll
       for (int e = 0; e < 16; ++e) dP[e] = -delta;
       if constexpr (NS > kG) {
@@ -184,7 +179,7 @@ window_dq_kernel(WindowBwdParams p) {
       }
       if (kb == (KB - 1) / 2 && tile + 1 < kt.n) {
         stage.store(tid, Kb[1 - B.value]);
-        load(vbase, p.ld_v, tile + 1);
+        load(stage, vbase, p.ld_v, tile + 1);
       }
     }
     if (tile + 1 < kt.n) stage.store(tid, Vb[1 - B.value]);
@@ -265,14 +260,11 @@ window_dq_few_kernel(WindowBwdParams p) {
     own();
     if (tile + 4 < kt.n) load(tile + 4);
     const int j0 = kt.first(tile, KT), jend = kt.end(tile);
-    const bool whole = j0 + KT <= jend && j0 + KT - 1 <= hi_a && (j0 >= lo_b || j0 + KT <= p.sinks);
+    const TileMask mask(j0, KT, jend, lo, hi, hi_a, lo_b, p.sinks, h32);
     f32x16 S = f32x16{}, dP;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int j = j0 + 8 * (e >> 2) + 4 * h32 + (e & 3);
-      if (!whole) S[e] = j < jend && j <= hi && (j >= lo || j < p.sinks) ? 0.f : -INFINITY;
-      dP[e] = -delta;
-    }
+    for (int e = 0; e < 16; ++e) dP[e] = -delta;
+    mask.hide(S, 0);
     frag A[NS], X[ND], D;
     read_along<DP>(Ks, 0, lane, A);
     S = product(A, Q, S);
@@ -313,7 +305,7 @@ window_dq_few_kernel(WindowBwdParams p) {
 // rows' positions; a hidden pair's score starts from -inf.
 template <typename T, int DP>
 __device__ __forceinline__ void key_block(const T* Qs, const T* Gs, const float* lse_s, const float* delta_s,
-                                          const int* pos_s, int r0, bool whole, int plo, int phi, float c,
+                                          const int* pos_s, int r0, bool cut_lo, bool cut_hi, int plo, int phi, float c,
                                           const typename Frag<T>::type (&K)[DP / 16],
                                           const typename Frag<T>::type (&V)[DP / 16], f32x16 (&dK)[DP / 32],
                                           f32x16 (&dV)[DP / 32], int lane, const uint32_t (&tr)[2]) {
@@ -323,13 +315,17 @@ __device__ __forceinline__ void key_block(const T* Qs, const T* Gs, const float*
   frag X[kG], Y[kG], W;
   read_part<DP, kG>(Qs, r0, 0, lane, X);
   f32x16 S = f32x16{}, dP;
-  if (!whole) {
+  if (cut_lo || cut_hi) {
 #pragma unroll
     for (int e4 = 0; e4 < 4; ++e4) {
       const int4 ps = *reinterpret_cast<const int4*>(pos_s + r0 + 8 * e4 + 4 * h32);
       const int pr[4] = {ps.x, ps.y, ps.z, ps.w};
+      if (cut_lo)
 #pragma unroll
-      for (int u = 0; u < 4; ++u) S[4 * e4 + u] = pr[u] >= plo && pr[u] <= phi ? 0.f : -INFINITY;
+        for (int u = 0; u < 4; ++u) S[4 * e4 + u] = pr[u] >= plo ? 0.f : -INFINITY;
+      if (cut_hi)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) S[4 * e4 + u] = pr[u] <= phi ? S[4 * e4 + u] : -INFINITY;
     }
   }
   if constexpr (NS > kG) {
@@ -521,10 +517,10 @@ window_dkv_kernel(WindowBwdParams p) {
     }
     if (tile + 1 < tiles) load(tile + 1);
     if (!live || pe < plo_a || pa > phi_b) continue;       // no row of the tile sees a key of the wave
-    const bool whole = pa >= plo_b && pe <= phi_a;
+    const bool cut_lo = pa < plo_b, cut_hi = pe > phi_a;
 #pragma unroll 1
     for (int r0 = 0; r0 < RT; r0 += 32)
-      key_block<T, DP>(Qs, Gs, lse_s, delta_s, pos_s, r0, whole, plo, phi, p.c, K, V, dK, dV, lane, tr);
+      key_block<T, DP>(Qs, Gs, lse_s, delta_s, pos_s, r0, cut_lo, cut_hi, plo, phi, p.c, K, V, dK, dV, lane, tr);
   }
   if (!mine) return;
   const bool more = p.split && j < p.sinks && tb < n;      // what the queries past the window add to a sink
@@ -635,8 +631,8 @@ window_dkv_few_kernel(WindowBwdParams p) {
       ++t0;
     }
     if (r + 4 * RT < rb) load(r + 4 * RT);
-    key_block<T, DP>(my.q, my.g, my.lse, my.delta, my.pos, 0, SINKS || (pa >= plo_b && pe <= phi_a), plo, phi, p.c, K, V,
-                     dK, dV, lane, tr);
+    key_block<T, DP>(my.q, my.g, my.lse, my.delta, my.pos, 0, !SINKS && pa < plo_b, !SINKS && pe > phi_a, plo, phi,
+                     p.c, K, V, dK, dV, lane, tr);
   }
   // the four waves' sums: dK, then dV, four channels per thread and turn
   constexpr int kTurns = 32 * DP / 4 / 256 > 0 ? 32 * DP / 4 / 256 : 1;

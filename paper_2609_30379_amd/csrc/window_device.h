@@ -299,5 +299,41 @@ struct KeyTiles {
   __device__ __forceinline__ int end(int t) const { return t < n_sink ? sink_end : hi; }
 };
 
+// Which keys of a tile (first key j0, keys below jend) a lane's row does not see.
+// Key offsets of an accumulator's elements are constants, so each bound that cuts
+// the tile costs a comparison and a selection per score; which ones do is the same
+// for the whole wave (hi_a, lo_b: the first row's last key, the last row's first).
+// Only a tile that holds both sinks and keys before the window needs a third.
+struct TileMask {
+  bool cut_hi, cut_lo, mixed;
+  int hi, lo, sink;              // relative to the lane's first key offset
+  __device__ __forceinline__ TileMask(int j0, int kt, int jend, int row_lo, int row_hi, int hi_a, int lo_b, int sinks, int h32) {
+    cut_hi = j0 + kt - 1 > min(hi_a, jend - 1);
+    cut_lo = j0 < lo_b && jend > sinks && j0 + kt > sinks;
+    mixed = j0 < sinks;
+    const int base = j0 + 4 * h32;
+    hi = min(row_hi, jend - 1) - base;
+    lo = row_lo - base;
+    sink = sinks - base;
+  }
+  __device__ __forceinline__ void hide(f32x16& s, int kb) const {
+    if (cut_hi)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = 32 * kb + 8 * (e >> 2) + (e & 3) <= hi ? s[e] : -INFINITY;
+    if (cut_lo) {
+      if (mixed) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int k = 32 * kb + 8 * (e >> 2) + (e & 3);
+          s[e] = k >= lo || k < sink ? s[e] : -INFINITY;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = 32 * kb + 8 * (e >> 2) + (e & 3) >= lo ? s[e] : -INFINITY;
+      }
+    }
+  }
+};
+
 }  // namespace win
 }  // namespace nt
