@@ -37,9 +37,13 @@ constexpr int kBlockShift = 7;                 // query rows per workgroup: 4 wa
 
 constexpr int kFewShift = 5;                   // query rows per workgroup of the few-rows kernel
 constexpr int kFewBlocks = 128;                // at most so many blocks of 128 rows: blocks of 32 instead
-// Key tiles of a split, at least (few rows: eight per wave), and workgroups that
-// a call with few blocks is cut into: two per compute unit.
-constexpr int kFewChunk = 32, kRowsChunk = 8, kSplitItems = 512;
+// Key tiles of a split, at least (few rows: eight per wave), and workgroups that a
+// call with few blocks is cut into: four per compute unit of few rows (64 tokens over
+// 500 .. 32000 keys, 8 key/value heads of 128: 816 us in 512, 769 in 1024, 796 in
+// 2048), else as many as are resident, three up to 64 channels (chunks of 300 .. 700
+// tokens over 8000 .. 30000, 16 heads of 64: 135 us in 512, 114 in 768, 122 in 1024)
+// and two past that.
+constexpr int kFewChunk = 32, kRowsChunk = 8, kFewItems = 1024, kRowsItems = 256;
 
 // One tile of KB x 32 keys against the wave's 32 rows: scores S become weights, O
 // and l are brought to the maximum in use.
@@ -274,7 +278,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2)
 window_few_kernel(WindowParams p) {
   typedef typename Frag<T>::type frag;
   typedef FewShape<T, DP> F;
-  constexpr int KT = F::KT, KB = KT / 32, NS = DP / 16, ND = DP / 32;
+  constexpr int KT = F::KT, KB = KT / 32, NS = DP / 16, ND = DP / 32, kG = NS < 4 ? NS : 4;
   union Shared {
     char tile[4][2][F::kTileBytes];
     struct {
@@ -348,9 +352,13 @@ window_few_kernel(WindowParams p) {
     f32x16 S[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-      frag A[NS];
-      read_along<DP>(Ks, 32 * kb, lane, A);
-      S[kb] = product(A, Q);
+      S[kb] = f32x16{};
+#pragma unroll
+      for (int ks = 0; ks < NS; ks += kG) {
+        frag A[kG];
+        read_part<DP, kG>(Ks, 32 * kb, ks, lane, A);
+        S[kb] = product_part<kG>(A, Q + ks, S[kb]);
+      }
     }
     online_softmax<KB, ND>(S, O, mx, l, p.c, mask);
 #pragma unroll
@@ -471,7 +479,8 @@ WindowPlan window_plan(const nt_window_args& a) {
   w.blocks = win::block_count(Lq.sum_n, Lq.batch, G, shift);
   int64_t total, most;
   count_tiles(a, shift, kt, &total, &most);
-  w.chunk = (int)std::max<int64_t>(w.few ? kFewChunk : kRowsChunk, (total + kSplitItems - 1) / kSplitItems);
+  const int items = w.few ? kFewItems : kRowsItems * (a.head_dim <= 64 ? 3 : 2);
+  w.chunk = (int)std::max<int64_t>(w.few ? kFewChunk : kRowsChunk, (total + items - 1) / items);
   w.splits = (int)std::max<int64_t>(1, (most + w.chunk - 1) / w.chunk);
   if (w.splits == 1) {
     w.chunk = INT32_MAX;

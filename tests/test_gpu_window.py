@@ -122,6 +122,16 @@ def test_long(dtype, d):
     run([900], [900], 2, 2, d, dtype)
 
 
+@pytest.mark.parametrize("batch", [1, 63, 64, 200, 5000])
+def test_many_samples(batch):
+    """Blocks find their sample: in one step of the lanes, in two, with empty samples between."""
+    rng = np.random.default_rng(batch)
+    n = [int(x) for x in rng.integers(0, 4, batch)]
+    n[batch // 2] = 150
+    m = [x + int(y) for x, y in zip(n, rng.integers(0, 3, batch))]
+    run(n, m, 2, 1, 8, "f32", left=9, sinks=1)
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.3, 2.0])
 def test_scales(scale):
     run([70, 9], [70, 9], 2, 1, 32, "bf16", left=30, sinks=1, scale=scale)
