@@ -6,6 +6,9 @@ pair block      the single-pair-single block of Eq. running-block, extended with
                 transition), over a packed [sum N_i^2, C] pair state.
 encoder layer   a pre-LayerNorm encoder layer on packed [sum N_i, C] tokens
                 with segmented attention and a per-sample mean pool.
+token model     token ids to embedding rows, layers with sliding-window
+                attention over the packed tokens, and the training step with
+                every gradient down to the embedding table.
 
 Workspaces (activation buffers and the ops' scratch) are allocated once per
 (layout, dims); a step allocates nothing.
@@ -522,3 +525,128 @@ class MechanismRun:
                 B.nt_layernorm_linear_backward(self.x, W["uv.w"], self.duv, dx=self.dx, accumulate_dx=True,
                                                dw=G["uv.w"], db=G["uv.b"], overwrite_weights=True, workspace=ws)
         return self.loss_s, self.loss_p, self.xt, self.Pt
+
+
+class TokenModel:
+    """A token model on a packed ragged batch as one training step: embedding
+    lookup, pre-LayerNorm layers with sliding-window attention (causal by
+    default, shared key/value heads, first tokens that stay visible), the
+    sample-weighted squared norm of the result as loss, and the backward of
+    every parameter, one C-ABI call per op.
+
+    Widths: C = heads * head_dim and hidden at most 1024.  Weight gradients are
+    overwritten every step (fp32); the loss stays on the device as per-sample
+    terms.  Every buffer, scratch included, is allocated here for the batch's
+    lengths: a step allocates nothing.  The layout holds N_i x 1 cells, so the
+    lengths are bounded by the tokens and not by their pairs."""
+
+    def __init__(self, lengths, params: dict, heads: int, kv_heads: int, head_dim: int, left: int = -1, right: int = 0,
+                 sinks: int = 0, device="cuda"):
+        self.H, self.K, self.d = heads, kv_heads, head_dim
+        self.lengths = [int(n) for n in lengths]
+        self.layout = lay = B.NestedLayout(self.lengths, cols=[1] * len(self.lengths))
+        self.W = to_device(params, "bf16", device)
+        self.layers = sum(1 for k in params if k.endswith(".qkv.w"))
+        T, C = lay.sum_n, heads * head_dim
+        Q, self.F = (heads + 2 * kv_heads) * head_dim, params["0.ffn1.w"].shape[0]
+        self.C, self.Q, self.scale = C, Q, math.sqrt(C)
+        self.window = dict(kv_heads=kv_heads, left=left, right=right, sinks=sinks)
+        e = lambda *shape, dt=torch.bfloat16: torch.empty(shape, dtype=dt, device=device)   # noqa: E731
+        f32 = torch.float32
+        # what the backward reads of every layer: its input, q|k|v, the attention's
+        # output and statistics, the state between its halves and the FFN's hidden rows
+        self.x = [e(T, C) for _ in range(self.layers + 1)]
+        self.mid = [e(T, C) for _ in range(self.layers)]
+        self.qkv = [e(T, Q) for _ in range(self.layers)]
+        self.o = [e(T, C) for _ in range(self.layers)]
+        self.lse = [e(heads, T, dt=f32) for _ in range(self.layers)]
+        self.h = [e(T, self.F) for _ in range(self.layers)]
+        self.loss, self.weight = e(lay.batch, dt=f32), torch.ones(lay.batch, dtype=f32, device=device)
+        self.dx, self.do, self.dh, self.dqkv = e(T, C), e(T, C), e(T, self.F), e(T, Q)
+        self.grads = {k: torch.empty(v.shape, dtype=f32, device=device) for k, v in self.W.items()}
+        need = [B.layernorm_linear_workspace_bytes(T, C, Q), B.layernorm_linear_workspace_bytes(T, C, self.F, epilogue="gelu"),
+                B.loss_workspace_bytes(lay),
+                B.window_attention_workspace_bytes(lay, heads, head_dim, **self.window),
+                B.window_attention_backward_workspace_bytes(lay, heads, head_dim, **self.window),
+                B.embedding_backward_workspace_bytes(T, self.W["embed"].shape[0], C),
+                self._backward_bytes(T, self.F, C, False, "residual"), self._backward_bytes(T, C, self.F, True, "gelu"),
+                self._backward_bytes(T, C, C, False, "residual"), self._backward_bytes(T, C, Q, True, "none")]
+        self.scratch = B.workspace_tensor(max(need), device)
+
+    @staticmethod
+    def _backward_bytes(rows, K, N, ln, epilogue):
+        """Workspace of a linear backward as step() calls it (the query looks at
+        which operands are there, not at what they hold)."""
+        import ctypes
+        a = B.LinearBwdArgs()
+        a.rows, a.c_in, a.c_out = rows, K, N
+        a.ldx, a.ld_dy, a.ld_dx = K, N, K
+        a.x_dtype = a.dx_dtype = B.NT_BF16
+        a.epilogue, a.overwrite_weights, a.accumulate_dx = B.EPILOGUES[epilogue], 1, int(ln)
+        some = ctypes.c_void_p(16)
+        a.x = a.w = a.dy = a.dx = a.dw = a.db = some
+        if ln:
+            a.ln_gamma = a.ln_beta = a.dgamma = a.dbeta = some
+        if epilogue == "gelu":
+            a.bias = some
+        n = ctypes.c_uint64()
+        B._check(B.load().nt_layernorm_linear_backward_workspace(ctypes.byref(a), ctypes.byref(n)))
+        return int(n.value)
+
+    def _qkv(self, t):
+        a, b = self.H * self.d, (self.H + self.K) * self.d
+        return t[:, :a], t[:, a:b], t[:, b:]
+
+    def forward(self, ids):
+        """ids: [sum N_i] token ids (int32 or int64; outside the table: padding rows of zeros)."""
+        lay, W, ws = self.layout, self.W, self.scratch
+        row = dict(layout=lay, level="singles")
+        with _op("embedding"):
+            B.nt_embedding(W["embed"], ids, self.x[0], scale=self.scale)
+        for i in range(self.layers):
+            x, w = self.x[i], (lambda k, _i=i: W[f"{_i}.{k}"])
+            with _op("qkv_proj"):
+                B.nt_layernorm_linear(x, w("qkv.w"), w("qkv.b"), self.qkv[i], ln=(w("ln1_g"), w("ln1_b")), workspace=ws, **row)
+            with _op("window_attention"):
+                B.nt_window_attention(lay, self.H, self.d, *self._qkv(self.qkv[i]), self.o[i], lse=self.lse[i], workspace=ws,
+                                      **self.window)
+            with _op("out_proj_residual"):
+                B.nt_layernorm_linear(self.o[i], w("o.w"), w("o.b"), self.mid[i], epilogue="residual", residual=x, **row)
+            with _op("ffn_up_gelu"):
+                B.nt_layernorm_linear(self.mid[i], w("ffn1.w"), w("ffn1.b"), self.h[i], ln=(w("ln2_g"), w("ln2_b")),
+                                      epilogue="gelu", workspace=ws, **row)
+            with _op("ffn_down_residual"):
+                B.nt_layernorm_linear(self.h[i], w("ffn2.w"), w("ffn2.b"), self.x[i + 1], epilogue="residual",
+                                      residual=self.mid[i], **row)
+        return self.x[-1]
+
+    def step(self, ids):
+        """Forward, loss and backward; returns (loss terms, the last state, gradients)."""
+        lay, W, G, ws = self.layout, self.W, self.grads, self.scratch
+        self.forward(ids)
+        with _op("loss"):
+            B.nt_weighted_square_loss(lay, "singles", self.x[-1], self.weight, 1.0 / max(1, self.C * lay.sum_n), self.loss,
+                                      dx=self.dx, workspace=ws)
+        for i in reversed(range(self.layers)):
+            w, g = (lambda k, _i=i: W[f"{_i}.{k}"]), (lambda k, _i=i: G[f"{_i}.{k}"])
+            over = dict(overwrite_weights=True, workspace=ws)
+            with _op("ffn_down_bwd"):
+                B.nt_layernorm_linear_backward(self.h[i], w("ffn2.w"), self.dx, epilogue="residual", dx=self.dh,
+                                               dw=g("ffn2.w"), db=g("ffn2.b"), **over)
+            with _op("ffn_up_bwd"):
+                B.nt_layernorm_linear_backward(self.mid[i], w("ffn1.w"), self.dh, ln=(w("ln2_g"), w("ln2_b")),
+                                               bias=w("ffn1.b"), epilogue="gelu", dx=self.dx, accumulate_dx=True,
+                                               dw=g("ffn1.w"), db=g("ffn1.b"), dgamma=g("ln2_g"), dbeta=g("ln2_b"), **over)
+            with _op("out_proj_bwd"):
+                B.nt_layernorm_linear_backward(self.o[i], w("o.w"), self.dx, epilogue="residual", dx=self.do, dw=g("o.w"),
+                                               db=g("o.b"), **over)
+            with _op("window_attention_bwd"):
+                B.nt_window_attention_backward(lay, self.H, self.d, *self._qkv(self.qkv[i]), self.o[i], self.lse[i], self.do,
+                                               *self._qkv(self.dqkv), workspace=ws, **self.window)
+            with _op("qkv_proj_bwd"):
+                B.nt_layernorm_linear_backward(self.x[i], w("qkv.w"), self.dqkv, ln=(w("ln1_g"), w("ln1_b")), dx=self.dx,
+                                               accumulate_dx=True, dw=g("qkv.w"), db=g("qkv.b"), dgamma=g("ln1_g"),
+                                               dbeta=g("ln1_b"), **over)
+        with _op("embedding_bwd"):
+            B.nt_embedding_backward(ids, self.dx, G["embed"], scale=self.scale, workspace=ws)
+        return self.loss, self.x[-1], G

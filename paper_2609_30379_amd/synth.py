@@ -21,6 +21,7 @@ import numpy as np
 __all__ = [
     "Workload", "WORKLOADS", "lengths_for", "tensor_rng", "snap_bf16",
     "pair_block_params", "encoder_layer_params", "normal", "cols_for", "mechanism_params", "mechanism_gains",
+    "token_model_params",
 ]
 
 
@@ -252,6 +253,25 @@ def encoder_layer_params(w: Workload, seed: int | None = None) -> dict:
     p["ln2_g"], p["ln2_b"] = _ln(seed, "enc.ln2", c)
     p["ffn1.w"], p["ffn1.b"] = _linear(seed, "enc.ffn1", w.hidden, c, g["ffn1"], dt)
     p["ffn2.w"], p["ffn2.b"] = _linear(seed, "enc.ffn2", c, w.hidden, g["ffn2"], dt)
+    return p
+
+
+def token_model_params(vocab: int, layers: int, heads: int, kv_heads: int, head_dim: int, hidden: int, seed: int = 0,
+                       dtype: str = "bf16") -> dict:
+    """Random-init weights of a token model: the embedding table (rows of norm
+    about one half once scaled by sqrt C), then per layer the pre-normalised
+    q|k|v projection with kv_heads key/value heads, the output projection and the
+    GELU feed-forward."""
+    c = heads * head_dim
+    p = {"embed": normal(seed, "tok.embed", (vocab, c), 0.5 / np.sqrt(c), dtype)}
+    for i in range(layers):
+        pre = f"tok{i}."
+        p[f"{i}.ln1_g"], p[f"{i}.ln1_b"] = _ln(seed, pre + "ln1", c)
+        p[f"{i}.qkv.w"], p[f"{i}.qkv.b"] = _linear(seed, pre + "qkv", (heads + 2 * kv_heads) * head_dim, c, 1.0, dtype)
+        p[f"{i}.o.w"], p[f"{i}.o.b"] = _linear(seed, pre + "o", c, c, 0.5, dtype)
+        p[f"{i}.ln2_g"], p[f"{i}.ln2_b"] = _ln(seed, pre + "ln2", c)
+        p[f"{i}.ffn1.w"], p[f"{i}.ffn1.b"] = _linear(seed, pre + "ffn1", hidden, c, 1.0, dtype)
+        p[f"{i}.ffn2.w"], p[f"{i}.ffn2.b"] = _linear(seed, pre + "ffn2", c, hidden, 0.5, dtype)
     return p
 
 

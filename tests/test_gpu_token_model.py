@@ -1,0 +1,107 @@
+"""The token model's training step (embedding, layers with window attention, loss,
+every gradient) against the same model in float64 autograd on the CPU.
+
+Bars: normwise.  Every stored bf16 tensor on the way from the parameters to a
+gradient is off by at most 2^-8 of its elements (half a step); a layer stores six
+forward (q|k|v, o, mid, h, x, and the normalised rows of each half count as one)
+and six backward, so after L layers a gradient's relative error is at most
+(12 L + 2) 2^-8 where each operation passes relative errors on without growth, as
+the residual stream and the normalisations do; the loss alone (L layers forward,
+squared) 2 (6 L + 1) 2^-8."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import tokens as T
+from paper_2609_30379_amd import synth
+
+from .gpu_util import host
+
+pytestmark = pytest.mark.gpu
+
+
+def reference(params, ids, lengths, H, K, d, left, right, sinks):
+    """(loss per sample, last state, gradients) in float64."""
+    import torch
+    P = {k: torch.tensor(v, dtype=torch.float64, requires_grad=True) for k, v in params.items()}
+    C, G, scale = H * d, H // K, math.sqrt(H * d)
+    inside = torch.tensor((ids >= 0) & (ids < params["embed"].shape[0]))
+    x = P["embed"][torch.tensor(np.where(inside, ids, 0))] * scale * inside[:, None]
+
+    def norm(x, g, b):
+        m, v = x.mean(1, keepdim=True), x.var(1, unbiased=False, keepdim=True)
+        return (x - m) / torch.sqrt(v + 1e-5) * g + b
+
+    layers = sum(1 for k in params if k.endswith(".qkv.w"))
+    for i in range(layers):
+        w = lambda k: P[f"{i}.{k}"]   # noqa: E731
+        qkv = norm(x, w("ln1_g"), w("ln1_b")) @ w("qkv.w").T + w("qkv.b")
+        q, k, v = qkv[:, :C].view(-1, H, d), qkv[:, C:C + K * d].view(-1, K, d), qkv[:, C + K * d:].view(-1, K, d)
+        rows, a = [], 0
+        for n in lengths:
+            seen = torch.tensor(T.visible(n, n, left, right, sinks))
+            o = []
+            for h in range(H):
+                s = q[a:a + n, h] @ k[a:a + n, h // G].T / math.sqrt(d)
+                o.append(torch.softmax(s.masked_fill(~seen, -math.inf), 1) @ v[a:a + n, h // G])
+            rows.append(torch.cat(o, 1) if n else torch.zeros((0, C), dtype=torch.float64))
+            a += n
+        mid = x + torch.cat(rows) @ w("o.w").T + w("o.b")
+        u = norm(mid, w("ln2_g"), w("ln2_b")) @ w("ffn1.w").T + w("ffn1.b")
+        x = mid + (0.5 * u * (1 + torch.erf(u / math.sqrt(2.0)))) @ w("ffn2.w").T + w("ffn2.b")
+    per = torch.stack([t.square().sum() for t in torch.split(x, lengths)]) / (C * sum(lengths))
+    per.sum().backward()
+    return per.detach().numpy(), x.detach().numpy(), {k: v.grad.numpy() for k, v in P.items()}
+
+
+@pytest.mark.parametrize("lengths,H,K,d,hidden,layers,window", [
+    ([37, 0, 90, 1, 129], 4, 2, 32, 256, 2, dict(left=24, right=0, sinks=2)),
+    ([64, 200], 2, 2, 64, 128, 1, dict(left=16, right=16, sinks=1)),
+    ([300, 5], 6, 1, 64, 512, 1, dict(left=-1, right=0, sinks=0)),
+])
+def test_training_step(lengths, H, K, d, hidden, layers, window):
+    import torch
+    from paper_2609_30379_amd import blocks
+    vocab = 50
+    params = synth.token_model_params(vocab, layers, H, K, d, hidden)
+    ids = np.random.default_rng(3).integers(0, vocab, sum(lengths))
+    ids[::17] = -1                                         # padding tokens
+    model = blocks.TokenModel(lengths, params, H, K, d, **window)
+    dev_ids = torch.tensor(ids, device="cuda")
+    loss, x, grads = model.step(dev_ids)
+    first = {k: host(v) for k, v in grads.items()}
+    ref_loss, ref_x, ref = reference(params, ids, lengths, H, K, d, **window)
+    bar = (12 * layers + 2) * 2.0 ** -8
+    far = lambda a, b: float(np.linalg.norm(a - b) / np.linalg.norm(b))   # noqa: E731
+    assert far(host(loss), ref_loss) <= 2 * (6 * layers + 1) * 2.0 ** -8
+    assert far(host(x), ref_x) <= bar
+    for k, g in first.items():
+        assert np.isfinite(g).all() and far(g, ref[k]) <= bar, (k, far(g, ref[k]))
+    unused = np.setdiff1d(np.arange(vocab), ids)
+    assert not first["embed"][unused].any()
+    model.step(dev_ids)
+    assert all(np.array_equal(first[k], host(v)) for k, v in grads.items())
+
+
+def test_captured_step_replays_with_new_tokens():
+    """A whole step in a graph, replayed on other tokens, with eager work in between."""
+    import torch
+    from paper_2609_30379_amd import blocks
+    lengths, H, K, d = [40, 130, 3], 4, 2, 32
+    params = synth.token_model_params(60, 1, H, K, d, 128)
+    model = blocks.TokenModel(lengths, params, H, K, d, left=20, sinks=2)
+    eager = blocks.TokenModel(lengths, params, H, K, d, left=20, sinks=2)
+    ids = torch.randint(0, 60, (sum(lengths),), device="cuda")
+    model.step(ids)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        model.step(ids)
+    for _ in range(3):
+        ids.copy_(torch.randint(-1, 60, ids.shape, device="cuda"))
+        graph.replay()
+        got = [host(model.loss)] + [host(v) for v in model.grads.values()]
+        eager.step(ids)
+        want = [host(eager.loss)] + [host(v) for v in eager.grads.values()]
+        assert all(np.array_equal(a, b) for a, b in zip(got, want))
