@@ -677,7 +677,7 @@ typedef struct {
   int32_t left;                /* >= 0, or -1                                     */
   int32_t right;               /* >= 0, or -1                                     */
   int32_t sinks;               /* >= 0                                            */
-  float scale;                 /* softmax scale, finite                           */
+  float scale;                 /* softmax scale, |scale| <= 1e38                  */
   nt_dtype dtype;              /* of q, k, v, o and of dout, dq, dk, dv           */
   const void* q;               /* [sum N, heads * head_dim]                       */
   int64_t ld_q;
@@ -692,7 +692,8 @@ typedef struct {
   const int32_t* kv_lengths;   /* see above                                       */
   void* workspace;
   uint64_t workspace_bytes;
-  /* nt_window_attention_backward only (o and lse are the forward's) */
+  /* nt_window_attention_backward only (o and lse are the forward's; dq, dk and dv
+   * must not overlap the operands) */
   const void* dout;            /* gradient of o                                   */
   int64_t ld_dout;
   void* dq;                    /* as q, overwritten                               */
@@ -704,7 +705,8 @@ typedef struct {
 } nt_window_args;
 
 /* Errors: NT_ERR_INVALID_ARG (NULL, sizes, strides, alignment, left or right
- * below -1, a layout of another device, a missing or too small workspace),
+ * below -1, an output that is an operand, a layout of another device, a missing
+ * or too small workspace),
  * NT_ERR_LAYOUT_MISMATCH (batch sizes differ), NT_ERR_UNSUPPORTED (head_dim, more
  * than 65536 heads),
  * NT_ERR_OVERFLOW (a sample of 2^30 tokens or more), NT_ERR_HIP.             */

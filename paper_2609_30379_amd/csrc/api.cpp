@@ -834,11 +834,13 @@ nt_status window_operands(const nt_window_args& a) {
   const int ve = vec_elems(a.dtype);
   const int64_t cq = (int64_t)a.heads * a.head_dim, ck = (int64_t)a.kv_heads * a.head_dim;
   const int64_t nq = a.q_layout->sum_n, nk = a.kv_layout->sum_n;
-  if (!(a.scale - a.scale == 0.f)) return nt::fail(NT_ERR_INVALID_ARG, "scale must be finite");
+  if (!(a.scale >= -1e38f && a.scale <= 1e38f)) return nt::fail(NT_ERR_INVALID_ARG, "scale must be finite, at most 1e38");
   if (nt_status st = matrix_operand(a.q, a.ld_q, cq, nq, ve, "q")) return st;
   if (nt_status st = matrix_operand(a.k, a.ld_k, ck, nk, ve, "k")) return st;
   if (nt_status st = matrix_operand(a.v, a.ld_v, ck, nk, ve, "v")) return st;
   if (nt_status st = matrix_operand(a.o, a.ld_o, cq, nq, ve, "o")) return st;
+  if (nq > 0 && (a.o == a.q || a.o == a.k || a.o == a.v))
+    return nt::fail(NT_ERR_INVALID_ARG, "o must not alias q, k or v");
   if (a.lse && ((reinterpret_cast<uintptr_t>(a.lse) & 3u) || a.ld_lse < nq))
     return nt::fail(NT_ERR_INVALID_ARG, "lse must be 4-byte aligned with ld_lse >= the query rows");
   if (nt_status st = on_current_device(a.q_layout)) return st;
@@ -906,6 +908,9 @@ nt_status nt_window_attention_backward(const nt_window_args* args, void* stream)
   if (nt_status st = matrix_operand(a.dq, a.ld_dq, cq, nq, ve, "dq")) return st;
   if (nt_status st = matrix_operand(a.dk, a.ld_dk, ck, nk, ve, "dk")) return st;
   if (nt_status st = matrix_operand(a.dv, a.ld_dv, ck, nk, ve, "dv")) return st;
+  for (const void* out : {(const void*)(nq ? a.dq : nullptr), (const void*)(nk ? a.dk : nullptr), (const void*)(nk ? a.dv : nullptr)})
+    if (out && (out == a.q || out == a.k || out == a.v || out == a.o || out == a.dout))
+      return nt::fail(NT_ERR_INVALID_ARG, "dq, dk and dv must not alias the operands");
   if (nq == 0 && nk == 0) return NT_OK;
   if (nt_status st = need_workspace(nt::window_backward_workspace_bytes(a), a.workspace, a.workspace_bytes,
                                     "nt_window_attention_backward_workspace"))

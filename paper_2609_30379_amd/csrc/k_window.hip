@@ -481,7 +481,11 @@ WindowPlan window_plan(const nt_window_args& a) {
   count_tiles(a, shift, kt, &total, &most);
   const int items = w.few ? kFewItems : kRowsItems * (a.head_dim <= 64 ? 3 : 2);
   w.chunk = (int)std::max<int64_t>(w.few ? kFewChunk : kRowsChunk, (total + items - 1) / items);
-  w.splits = (int)std::max<int64_t>(1, (most + w.chunk - 1) / w.chunk);
+  // every block gets the splits of the longest one, most of them empty where lengths
+  // differ much: bounded, so that empty workgroups never outweigh the work
+  const int64_t room = std::max<int64_t>(1, 16 * (int64_t)items / std::max<int64_t>(1, w.blocks * a.kv_heads));
+  w.splits = (int)std::max<int64_t>(1, std::min(room, (most + w.chunk - 1) / w.chunk));
+  w.chunk = (int)std::max<int64_t>(w.chunk, (most + w.splits - 1) / w.splits);
   if (w.splits == 1) {
     w.chunk = INT32_MAX;
     return w;

@@ -32,7 +32,8 @@ struct WindowBwdParams {
   bool narrow;
   // gradients of the sinks from the queries past their window (window_sink_kernel)
   int split;                     // done apart, in pieces of `piece` rows
-  int subs, pieces, piece;       // blocks of 32 sinks, most pieces of a sample, rows per piece
+  int subs, pieces;              // blocks of 32 sinks, most pieces of a sample
+  int64_t piece;                 // rows per piece
   float *sink_part, *sink_sum;   // [batch][kv_heads][subs][pieces][2][32][DP], [batch][kv_heads][subs][2][32][DP]
 };
 
@@ -590,7 +591,7 @@ window_dkv_few_kernel(WindowBwdParams p) {
   const int far = p.left >= 0 ? max(ta, window_end(blk_end, p.left, off, n)) : n;
   int64_t ra, rb;
   if (SINKS) {
-    ra = (int64_t)far * p.group + (int64_t)piece * p.piece;
+    ra = (int64_t)far * p.group + piece * p.piece;
     rb = min((int64_t)n * p.group, ra + p.piece);
   } else {
     ra = (int64_t)ta * p.group;
@@ -703,7 +704,8 @@ sink_sum_kernel(WindowBwdParams p) {
 // sums stay bounded.
 constexpr int kSinkPiece = 512, kSinkItems = 1024;
 struct SinkPlan {
-  int split, subs, pieces, piece, dp;
+  int split, subs, pieces, dp;
+  int64_t piece;
   size_t delta_bytes, part_bytes, sum_bytes;
 };
 SinkPlan sink_plan(const nt_window_args& a) {
@@ -724,7 +726,7 @@ SinkPlan sink_plan(const nt_window_args& a) {
   s.subs = (a.sinks + 31) / 32;
   const int64_t blocks = (int64_t)Lq.batch * a.kv_heads * s.subs;
   const int64_t want = std::max<int64_t>(1, std::min(rows / kSinkPiece, kSinkItems / blocks));
-  s.piece = (int)((rows + want - 1) / want + 127) / 128 * 128;
+  s.piece = ((rows + want - 1) / want + 127) / 128 * 128;
   s.pieces = (int)((rows + s.piece - 1) / s.piece);
   s.part_bytes = (size_t)blocks * s.pieces * 64 * s.dp * sizeof(float);
   s.sum_bytes = (size_t)blocks * 64 * s.dp * sizeof(float);

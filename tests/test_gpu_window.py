@@ -278,3 +278,38 @@ def test_single_tokens_give_a_prompts_rows():
                               kv_lengths=torch.tensor([t + 1], dtype=torch.int32, device="cuda"), **kw)
         # two fp32 orders of the same sums, each within fp_rel of it
         assert float((r - o[t:t + 1]).abs().max()) <= 2 * 2.0 ** -22 * (d + 16) * 8 * float(v.abs().max())
+
+
+def test_outputs_that_are_operands_are_refused():
+    import torch
+    from paper_2609_30379_amd import binding as B
+    lay = layout([8])
+    x = [torch.zeros((8, 32), dtype=torch.bfloat16, device="cuda") for _ in range(8)]
+    lse = torch.zeros((1, 8), device="cuda")
+    with pytest.raises(B.NtError):
+        B.nt_window_attention(lay, 1, 32, x[0], x[1], x[2], x[2])
+    for bad in range(3):
+        g = [x[5], x[6], x[7]]
+        g[bad] = x[bad]
+        with pytest.raises(B.NtError):
+            B.nt_window_attention_backward(lay, 1, 32, x[0], x[1], x[2], x[3], lse, x[4], *g)
+    with pytest.raises(ValueError):
+        B.nt_window_attention(lay, 1, 32, x[0].cpu(), x[1], x[2], x[3])
+    with pytest.raises(ValueError):
+        B.nt_window_attention(lay, 1, 32, x[0], x[1], x[2], x[3][:7])
+    with pytest.raises(ValueError):
+        B.nt_window_attention(lay, 1, 32, x[0], x[1].float(), x[2], x[3])
+
+
+def test_keys_without_any_query_get_zero_gradients():
+    import torch
+    from paper_2609_30379_amd import binding as B
+    ql, kl = layout([0, 0]), layout([5, 200])
+    q = torch.zeros((0, 64), dtype=torch.bfloat16, device="cuda")
+    k = torch.ones((205, 32), dtype=torch.bfloat16, device="cuda")
+    v, lse = k.clone(), torch.zeros((2, 0), device="cuda")
+    dk, dv = torch.full_like(k, float("nan")), torch.full_like(k, float("nan"))
+    B.nt_window_attention(ql, 2, 32, q, k, v, q.clone(), kv_layout=kl, kv_heads=1, lse=lse)
+    B.nt_window_attention_backward(ql, 2, 32, q, k, v, q.clone(), lse, q.clone(), q.clone(), dk, dv, kv_layout=kl, kv_heads=1,
+                                   left=3, sinks=1)
+    assert not bool(dk.any()) and not bool(dv.any())

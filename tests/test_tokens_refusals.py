@@ -20,7 +20,8 @@ def window_args(**kw):
     KEEP.append(lay)
     a.q_layout = lay.handle
     a.heads, a.kv_heads, a.head_dim, a.left, a.right, a.sinks, a.scale, a.dtype = 4, 2, 32, 3, 0, 1, 0.2, B.NT_BF16
-    a.q = a.k = a.v = a.o = a.dout = a.dq = a.dk = a.dv = P
+    a.q = a.k = a.v = a.dout = P
+    a.o, a.dq, a.dk, a.dv = 2 * P, 3 * P, 4 * P, 5 * P
     a.ld_q = a.ld_o = a.ld_dout = a.ld_dq = 128
     a.ld_k = a.ld_v = a.ld_dk = a.ld_dv = 64
     a.lse, a.ld_lse = P, 12
@@ -61,6 +62,8 @@ WINDOW = [
     (dict(ld_v=60), B.NT_ERR_INVALID_ARG, "v's row stride"),
     (dict(ld_v=68), B.NT_ERR_INVALID_ARG, "v's row stride"),
     (dict(ld_o=120), B.NT_ERR_INVALID_ARG, "o's row stride"),
+    (dict(scale=2e38), B.NT_ERR_INVALID_ARG, "scale"),
+    (dict(o=P), B.NT_ERR_INVALID_ARG, "alias"),
     (dict(ld_lse=11), B.NT_ERR_INVALID_ARG, "lse"),
     (dict(lse=P + 2), B.NT_ERR_INVALID_ARG, "lse"),
 ]
