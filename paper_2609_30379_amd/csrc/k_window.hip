@@ -156,14 +156,13 @@ window_rows_kernel(WindowParams p) {
   const T* vbase = (const T*)p.v + (int64_t)hk * p.d;
   // The next tile's keys travel while the scores of this one are computed, its
   // values while the weights are applied: one set of registers for both.
-  Stage<T, DP, KT, 256> stage;
+  Stage<T, DP, KT, 256> stage, values;
   auto load = [&](auto& to, const T* base, int64_t ld, int tile) {
     const int j0 = kt.first(tile, KT), cnt = min(kt.end(tile) - j0, KT);
     to.load(tid, base + (int64_t)(k0 + j0) * ld, ld, cnt, p.d, p.narrow);
   };
   const int first = split * p.chunk, end = min(kt.n, first + p.chunk);
   if (first < end) {
-    Stage<T, DP, KT, 256> values;                          // both in flight at once
     load(stage, kbase, p.ld_k, first);
     load(values, vbase, p.ld_v, first);
     stage.store(tid, Kb[0]);
@@ -174,7 +173,10 @@ window_rows_kernel(WindowParams p) {
   auto body = [&](auto B, int tile) {
     __syncthreads();
     const T *Ks = Kb[B.value], *Vs = Vb[B.value];
-    if (tile + 1 < end) load(stage, kbase, p.ld_k, tile + 1);
+    if (tile + 1 < end) {
+      load(stage, kbase, p.ld_k, tile + 1);
+      if (KB == 1) load(values, vbase, p.ld_v, tile + 1);
+    }
     const int j0 = kt.first(tile, KT), jend = kt.end(tile);
     // unless nothing of the tile is visible to any row of the wave
     const bool seen = live && j0 <= hi_b && (min(j0 + KT, jend) > lo_a || j0 < p.sinks);
@@ -184,6 +186,7 @@ window_rows_kernel(WindowParams p) {
     f32x16 S[KB];
     frag X[kG], Y[kG];
     if (seen) {
+      __builtin_amdgcn_s_setprio(1);
       read_part<DP, kG>(Ks, 0, 0, lane, X);
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
@@ -207,13 +210,15 @@ window_rows_kernel(WindowParams p) {
             for (int k = 0; k < kG; ++k) X[k] = Y[k];
         }
       }
+      __builtin_amdgcn_s_setprio(0);
       online_softmax<KB, ND>(S, O, mx, l, p.c, mask);
     }
     if (tile + 1 < end) {
       stage.store(tid, Kb[1 - B.value]);
-      load(stage, vbase, p.ld_v, tile + 1);
+      if (KB > 1) load(stage, vbase, p.ld_v, tile + 1);
     }
     if (seen) {
+      __builtin_amdgcn_s_setprio(1);
       read_across<DP>(Vs, 0, lane, tr, X);
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
@@ -228,8 +233,9 @@ window_rows_kernel(WindowParams p) {
         pin();
         add_products(Y, P, O);
       }
+      __builtin_amdgcn_s_setprio(0);
     }
-    if (tile + 1 < end) stage.store(tid, Vb[1 - B.value]);
+    if (tile + 1 < end) (KB > 1 ? stage : values).store(tid, Vb[1 - B.value]);
   };
   for (int tile = first; tile < end; tile += 2) {
     body(std::integral_constant<int, 0>{}, tile);

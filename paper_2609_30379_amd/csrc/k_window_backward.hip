@@ -9,7 +9,6 @@
 // the products, so P and dS go from accumulators into the next operand in
 // registers.
 #include <algorithm>
-#include <type_traits>
 
 #include "window_device.h"
 
@@ -82,7 +81,7 @@ template <typename T, int DP>
 __global__ void __launch_bounds__(256, DP == 32 ? 3 : DP == 128 && sizeof(T) == 4 ? 1 : 2)
 window_dq_kernel(WindowBwdParams p) {
   typedef typename Frag<T>::type frag;
-  constexpr int KT = sizeof(T) == 2 ? 64 : 32, KB = KT / 32, NS = DP / 16, ND = DP / 32, kG = NS < 4 ? NS : 4;
+  constexpr int KT = sizeof(T) == 2 && DP < 128 ? 64 : 32, KB = KT / 32, NS = DP / 16, ND = DP / 32, kG = NS < 4 ? NS : 4;
   __shared__ __attribute__((aligned(16))) T Kb[2][KT * Tile<T, DP>::kLd];
   __shared__ __attribute__((aligned(16))) T Vb[2][KT * Tile<T, DP>::kLd];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h32 = lane >> 5;
@@ -120,23 +119,26 @@ window_dq_kernel(WindowBwdParams p) {
   const T* kbase = (const T*)p.k + (int64_t)hk * p.d;
   const T* vbase = (const T*)p.v + (int64_t)hk * p.d;
   // the next tile's keys travel during the first half of this one, its values
-  // during the second: one set of registers for both
-  Stage<T, DP, KT, 256> stage;
+  // during the second, through the same registers (tiles of 32 keys: both at once)
+  Stage<T, DP, KT, 256> stage, values;
   auto load = [&](auto& to, const T* base, int64_t ld, int tile) {
     const int j0 = kt.first(tile, KT), cnt = min(kt.end(tile) - j0, KT);
     to.load(tid, base + (int64_t)(k0 + j0) * ld, ld, cnt, p.d, p.narrow);
   };
   if (kt.n > 0) {
-    Stage<T, DP, KT, 256> values;                          // both in flight at once
     load(stage, kbase, p.ld_k, 0);
     load(values, vbase, p.ld_v, 0);
     stage.store(tid, Kb[0]);
     values.store(tid, Vb[0]);
   }
-  auto body = [&](auto B, int tile) {                      // one tile from buffer B, a constant
+  for (int tile = 0; tile < kt.n; ++tile) {
     __syncthreads();
-    const T *Ks = Kb[B.value], *Vs = Vb[B.value];
-    if (tile + 1 < kt.n) load(stage, kbase, p.ld_k, tile + 1);
+    const int buf = tile & 1;
+    const T *Ks = Kb[buf], *Vs = Vb[buf];
+    if (tile + 1 < kt.n) {
+      load(stage, kbase, p.ld_k, tile + 1);
+      if (KB == 1) load(values, vbase, p.ld_v, tile + 1);
+    }
     const int j0 = kt.first(tile, KT), jend = kt.end(tile);
     const bool seen = live && j0 <= hi_b && (min(j0 + KT, jend) > lo_a || j0 < p.sinks);
     const TileMask mask(j0, KT, jend, lo, hi, hi_a, lo_b, p.sinks, h32);
@@ -179,15 +181,11 @@ window_dq_kernel(WindowBwdParams p) {
       add_products(Y, D, dQ);
       }
       if (kb == (KB - 1) / 2 && tile + 1 < kt.n) {
-        stage.store(tid, Kb[1 - B.value]);
-        load(stage, vbase, p.ld_v, tile + 1);
+        stage.store(tid, Kb[1 - buf]);
+        if (KB > 1) load(stage, vbase, p.ld_v, tile + 1);
       }
     }
-    if (tile + 1 < kt.n) stage.store(tid, Vb[1 - B.value]);
-  };
-  for (int tile = 0; tile < kt.n; tile += 2) {
-    body(std::integral_constant<int, 0>{}, tile);
-    if (tile + 1 < kt.n) body(std::integral_constant<int, 1>{}, tile + 1);
+    if (tile + 1 < kt.n) (KB > 1 ? stage : values).store(tid, Vb[1 - buf]);
   }
   if (!mine) return;
 #pragma unroll
