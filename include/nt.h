@@ -650,10 +650,10 @@ nt_status nt_layernorm_linear_backward_workspace(const nt_linear_bwd_args* args,
  *     s_j = scale q[eta_i + t, h] . k[kappa_i + j, h']
  *     o[eta_i + t, h] = sum_j softmax_j(s)_j v[kappa_i + j, h'],  lse = log sum_j exp(s_j)
  * over the visible keys.  A query that sees no key gets o = 0, lse = -inf and no
- * gradient.  Where a wave's 32 queries see only part of a tile of 64 (fp32: 32)
- * keys, the others of the tile enter with weight 0: their values must be finite.
- * Keys that no query of a block of 128 / (heads / kv_heads) queries sees, and
- * keys past kv_lengths, are never read as values and may hold anything.
+ * gradient.  All M_i keys and values and, in the backward, all operands must be
+ * finite: a key that some query does not see enters that query's sums with weight
+ * 0, which an infinite value or key turns into NaN.  Keys past kv_lengths and rows
+ * behind the last sample are never read and may hold anything.
  *   Layouts are used for their lengths alone.  Long samples need no pair state:
  *   nt_from_rect_lengths with every column count 1 describes N_i tokens without
  *   the N_i^2 cells that would overflow.
@@ -693,7 +693,7 @@ typedef struct {
   void* workspace;
   uint64_t workspace_bytes;
   /* nt_window_attention_backward only (o and lse are the forward's; dq, dk and dv
-   * must not overlap the operands) */
+   * must overlap neither the operands nor one another) */
   const void* dout;            /* gradient of o                                   */
   int64_t ld_dout;
   void* dq;                    /* as q, overwritten                               */
@@ -705,7 +705,7 @@ typedef struct {
 } nt_window_args;
 
 /* Errors: NT_ERR_INVALID_ARG (NULL, sizes, strides, alignment, left or right
- * below -1, an output that is an operand, a layout of another device, a missing
+ * below -1, an output that is an operand or another output, a layout of another device, a missing
  * or too small workspace),
  * NT_ERR_LAYOUT_MISMATCH (batch sizes differ), NT_ERR_UNSUPPORTED (head_dim, more
  * than 65536 heads),
@@ -729,8 +729,9 @@ nt_status nt_window_attention_backward_workspace(const nt_window_args* args, uin
  *   table   [vocab, C] row stride ld_table (table_dtype)
  *   ids     device, [rows], int32, or int64 with ids_are_64; element-aligned
  *   y       [rows, C] row stride ld_y (y_dtype, which may differ from the table's)
- *   C       a multiple of 8
- * Errors: NT_ERR_INVALID_ARG, NT_ERR_OVERFLOW (rows or vocab beyond int32).  */
+ *   C       a multiple of 8, at most 2^24
+ * Errors: NT_ERR_INVALID_ARG (also y equal to table), NT_ERR_OVERFLOW (rows or
+ * vocab beyond int32, C).                                                    */
 nt_status nt_embedding(const void* table, int64_t vocab, int64_t ld_table, nt_dtype table_dtype, const void* ids,
                        int32_t ids_are_64, int64_t rows, int32_t C, float scale, void* y, int64_t ld_y,
                        nt_dtype y_dtype, void* stream);

@@ -851,6 +851,7 @@ nt_status embedding_sizes(int64_t rows, int64_t vocab, int32_t C) {
   if (rows < 0 || vocab < 0) return nt::fail(NT_ERR_INVALID_ARG, "rows and vocab must be >= 0");
   if (rows > INT32_MAX || vocab >= INT32_MAX) return nt::fail(NT_ERR_OVERFLOW, "rows or vocab exceed int32");
   if (C <= 0 || C % 8) return nt::fail(NT_ERR_INVALID_ARG, "C must be a positive multiple of 8");
+  if (C > 1 << 24) return nt::fail(NT_ERR_OVERFLOW, "C beyond 2^24");
   return NT_OK;
 }
 
@@ -911,6 +912,8 @@ nt_status nt_window_attention_backward(const nt_window_args* args, void* stream)
   for (const void* out : {(const void*)(nq ? a.dq : nullptr), (const void*)(nk ? a.dk : nullptr), (const void*)(nk ? a.dv : nullptr)})
     if (out && (out == a.q || out == a.k || out == a.v || out == a.o || out == a.dout))
       return nt::fail(NT_ERR_INVALID_ARG, "dq, dk and dv must not alias the operands");
+  if ((nk && a.dk == a.dv) || (nq && nk && (a.dq == a.dk || a.dq == a.dv)))
+    return nt::fail(NT_ERR_INVALID_ARG, "dq, dk and dv must not alias one another");
   if (nq == 0 && nk == 0) return NT_OK;
   if (nt_status st = need_workspace(nt::window_backward_workspace_bytes(a), a.workspace, a.workspace_bytes,
                                     "nt_window_attention_backward_workspace"))
@@ -929,6 +932,7 @@ nt_status nt_embedding(const void* table, int64_t vocab, int64_t ld_table, nt_dt
   if (nt_status st = matrix_operand(table, ld_table, C, vocab, vec_elems(table_dtype), "table")) return st;
   if (nt_status st = matrix_operand(y, ld_y, C, rows, vec_elems(y_dtype), "y")) return st;
   if (rows == 0) return NT_OK;
+  if (y == table) return nt::fail(NT_ERR_INVALID_ARG, "y must not alias the table");
   return check_hip(nt::launch_embedding(table, vocab, ld_table, table_dtype, ids, ids_are_64, rows, C, scale, y, ld_y,
                                         y_dtype, static_cast<hipStream_t>(stream)),
                    "nt_embedding launch");
@@ -957,6 +961,7 @@ nt_status nt_embedding_backward(const void* ids, int32_t ids_are_64, int64_t row
   if (nt_status st = need_workspace(nt::embedding_backward_workspace_bytes(rows, vocab, C), workspace, workspace_bytes,
                                     "nt_embedding_backward_workspace"))
     return st;
+  if (rows > 0 && dtable == dy) return nt::fail(NT_ERR_INVALID_ARG, "dtable must not alias dy");
   return check_hip(nt::launch_embedding_backward(ids, ids_are_64, rows, vocab, C, dy, ld_dy, dtype, scale, dtable,
                                                  ld_dtable, table_dtype, accumulate, workspace,
                                                  static_cast<hipStream_t>(stream)),

@@ -109,7 +109,8 @@ struct SortParams {
   uint32_t vocab;
   const uint32_t *key_in, *row_in;
   uint32_t *key_out, *row_out;
-  uint32_t* hist;                // [tiles][bins]
+  uint32_t* hist;                // [tiles + 1][bins]: counts; or, scanned, those of the tiles before, and all
+  int scanned;
   int64_t rows;
   int tiles, shift, bits, passes;   // tiles, or ranges of ids
   uint32_t range;                // ids per range
@@ -286,6 +287,45 @@ sort_count_kernel(SortParams p) {
   for (int b = tid; b < bins; b += 256) p.hist[(int64_t)blockIdx.x * bins + b] = h[b];
 }
 
+// Every tile's counts become those of the tiles before it, and row `tiles` their
+// totals: where there are so many tiles that each of them adding up all counts
+// would cost more than this launch.  A workgroup has 64 digits, each of its 16
+// waves a sixteenth of the tiles.
+__global__ void __launch_bounds__(1024)
+sort_scan_kernel(SortParams p) {
+  __shared__ uint32_t sums[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bins = 1 << p.bits, own = (bins + 63) / 64;
+  if ((int)blockIdx.x >= own) {
+    clear_pieces(p, ((int64_t)blockIdx.x - own) * 16 + wave, ((int64_t)gridDim.x - own) * 16, lane);
+    return;
+  }
+  const int dg = blockIdx.x * 64 + lane, lo = (int)((int64_t)p.tiles * wave / 16), hi = (int)((int64_t)p.tiles * (wave + 1) / 16);
+  uint32_t* h = p.hist + min(dg, bins - 1);
+  uint32_t n = 0;
+#pragma unroll 8
+  for (int t = lo; t < hi; ++t) n += h[(int64_t)t * bins];
+  sums[wave][lane] = n;
+  __syncthreads();
+  uint32_t at = 0;
+  for (int w = 0; w < wave; ++w) at += sums[w][lane];
+  if (dg >= bins) return;
+  for (int t0 = lo; t0 < hi; t0 += 8) {
+    uint32_t c[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) c[u] = h[(int64_t)min(t0 + u, hi - 1) * bins];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (t0 + u < hi) h[(int64_t)(t0 + u) * bins] = at;
+      at += c[u];
+    }
+  }
+  if (wave == 15) {
+    uint32_t all = 0;
+    for (int w = 0; w < 16; ++w) all += sums[w][lane];
+    h[(int64_t)p.tiles * bins] = all;
+  }
+}
+
 template <int ITER>
 __global__ void __launch_bounds__(256)
 sort_scatter_kernel(SortParams p) {
@@ -309,7 +349,14 @@ sort_scatter_kernel(SortParams p) {
   for (int b = tid; b < 4 * kMaxBins; b += 256) (&wc[0][0])[b] = 0;
   // thread t has the digits 2 t and 2 t + 1: their totals, and the tiles before
   uint32_t t0 = 0, t1 = 0, b0 = 0, b1 = 0;
-  if (2 * tid < bins)
+  if (2 * tid < bins && p.scanned) {
+    const uint2 all = *reinterpret_cast<const uint2*>(p.hist + (int64_t)p.tiles * bins + 2 * tid);
+    const uint2 before = *reinterpret_cast<const uint2*>(p.hist + (int64_t)tile * bins + 2 * tid);
+    t0 = all.x;
+    t1 = all.y;
+    b0 = before.x;
+    b1 = before.y;
+  } else if (2 * tid < bins) {
 #pragma unroll 8
     for (int t = 0; t < p.tiles; ++t) {
       const uint2 c = *reinterpret_cast<const uint2*>(p.hist + (int64_t)t * bins + 2 * tid);
@@ -318,6 +365,7 @@ sort_scatter_kernel(SortParams p) {
       b0 += t < tile ? c.x : 0;
       b1 += t < tile ? c.y : 0;
     }
+  }
   const uint32_t incl = wave_scan(t0 + t1, lane);
   if (lane == 63) sums[wave] = incl;
   __syncthreads();
@@ -501,11 +549,19 @@ embedding_join_kernel(SumParams p, TG* __restrict__ dtable, int64_t ld) {
 }
 
 // Sorted rows per chunk: 32, and up to 128 where there are 2048 chunks or more all
-// the same; longer chunks leave fewer partial sums to add.
-int chunk_of(int64_t rows) { return rows < 1 << 17 ? 32 : rows < 1 << 18 ? 64 : 128; }
+// the same; longer chunks leave fewer partial sums to add.  At most 65536 chunks,
+// so that one token's run over all rows stays a short list of them.
+int chunk_of(int64_t rows) {
+  return rows < 1 << 17 ? 32 : rows < 1 << 18 ? 64 : (int)std::max<int64_t>(128, (rows + 65535) >> 16);
+}
 // Pairs per tile / 256: small tiles where few would leave the sort to a handful of
 // workgroups, large ones where every tile adds up the counts of many.
 int tile_iter(int64_t rows) { return rows <= 1 << 17 ? 4 : 16; }
+// From so many pairs on (98 tiles), the tiles' counts are summed by a launch of their
+// own (C = 64, 32000 ids, with and without it: 262144 tokens 99.5 and 96.5 us, 400000
+// 102 and 103, 524288 102 and 108, 4 million 357 and 438; 131072 tokens at C = 2048,
+// where the clearing decides, 595 and 590).
+constexpr int64_t kScanRows = 400000;
 
 struct Plan {
   bool small;
@@ -534,7 +590,7 @@ Plan plan(int64_t rows, int64_t vocab, int C) {
     s.key[k] = take((size_t)rows * 4);
     s.row[k] = take((size_t)rows * 4);
   }
-  s.hist = take(s.small ? 0 : (size_t)s.tiles * (1u << s.bits) * 4);
+  s.hist = take(s.small ? 0 : ((size_t)s.tiles + 1) * (1u << s.bits) * 4);
   s.part = take((size_t)s.chunks * 2 * C * 4);
   s.bytes = at;
   return s;
@@ -552,6 +608,7 @@ hipError_t backward(const void* ids, int wide, int64_t rows, int64_t vocab, int 
   sp.bits = pl.bits;
   sp.passes = pl.passes;
   sp.hist = (uint32_t*)(ws + pl.hist);
+  sp.scanned = rows >= kScanRows;
   // memory to clear: 4 KB pieces of a dense table, else its rows
   sp.fill = (char*)dtable;
   const bool dense = ld == C;
@@ -573,9 +630,9 @@ hipError_t backward(const void* ids, int wide, int64_t rows, int64_t vocab, int 
     if (hipError_t e = hipGetLastError()) return e;
   } else {
     last = (pl.passes - 1) & 1;
-    const int steps = 2 * pl.passes;                     // launches that share the clearing
+    const int each = sp.scanned ? 3 : 2, steps = each * pl.passes;   // launches that share the clearing
     for (int k = 0; k < steps; ++k) {
-      const int pass = k / 2;
+      const int pass = k / each, what = k % each == 0 ? 0 : k % each + (3 - each);   // 0 counts, 1 scans, 2 scatters
       sp.ids = pass ? nullptr : ids;
       sp.key_in = (uint32_t*)(ws + pl.key[(pass + 1) & 1]);
       sp.row_in = (uint32_t*)(ws + pl.row[(pass + 1) & 1]);
@@ -584,13 +641,15 @@ hipError_t backward(const void* ids, int wide, int64_t rows, int64_t vocab, int 
       sp.shift = pass * pl.bits;
       sp.fill_lo = pieces * k / steps;
       sp.fill_hi = pieces * (k + 1) / steps;
-      const int grid = pl.tiles + (int)std::min<int64_t>((sp.fill_hi - sp.fill_lo + 3) / 4, 2048);
-      if (k & 1) {
-        if (pl.iter == 4) sort_scatter_kernel<4><<<grid, 256, 0, s>>>(sp);
-        else sort_scatter_kernel<16><<<grid, 256, 0, s>>>(sp);
+      const int waves = what == 1 ? 16 : 4, clear = (int)std::min<int64_t>((sp.fill_hi - sp.fill_lo + waves - 1) / waves, 8192 / waves);
+      if (what == 0) {
+        if (pl.iter == 4) sort_count_kernel<4><<<pl.tiles + clear, 256, 0, s>>>(sp);
+        else sort_count_kernel<16><<<pl.tiles + clear, 256, 0, s>>>(sp);
+      } else if (what == 1) {
+        sort_scan_kernel<<<((1 << pl.bits) + 63) / 64 + clear, 1024, 0, s>>>(sp);
       } else {
-        if (pl.iter == 4) sort_count_kernel<4><<<grid, 256, 0, s>>>(sp);
-        else sort_count_kernel<16><<<grid, 256, 0, s>>>(sp);
+        if (pl.iter == 4) sort_scatter_kernel<4><<<pl.tiles + clear, 256, 0, s>>>(sp);
+        else sort_scatter_kernel<16><<<pl.tiles + clear, 256, 0, s>>>(sp);
       }
       if (hipError_t e = hipGetLastError()) return e;
     }

@@ -278,13 +278,13 @@ hipError_t launch_triangle_backward(const nt_layout& L, int direction, int C, co
 
 // Window attention (k_window.hip, k_window_backward.hip).  The arguments are
 // checked and left, right and sinks brought within the samples' lengths by the
-// caller (normalised_window).
+// caller (window_sizes in api.cpp).
 size_t window_workspace_bytes(const nt_window_args& a);
 hipError_t launch_window(const nt_window_args& a, hipStream_t s);
 size_t window_backward_workspace_bytes(const nt_window_args& a);
 hipError_t launch_window_backward(const nt_window_args& a, hipStream_t s);
 
-// Embedding (k_embedding.hip): vocab and rows within int32, C % 8 == 0.
+// Embedding (k_embedding.hip): vocab and rows within int32, C % 8 == 0, C <= 2^24.
 size_t embedding_backward_workspace_bytes(int64_t rows, int64_t vocab, int C);
 hipError_t launch_embedding(const void* table, int64_t vocab, int64_t ld_table, nt_dtype table_dtype, const void* ids,
                             int wide, int64_t rows, int C, float scale, void* y, int64_t ld_y, nt_dtype y_dtype,

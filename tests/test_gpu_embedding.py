@@ -121,3 +121,33 @@ def test_captured_gradient_replays():
         got = host(g)
         B.nt_embedding_backward(ids, dy, want)
         assert np.array_equal(got, host(want))
+
+
+@pytest.mark.parametrize("rows,vocab", [(524288, 300), (524289, 70001), (600001, 1), (9000001, 70001), (8500000, 2)])
+def test_gradient_of_many_tokens(rows, vocab):
+    """Sorts of more than 128 tiles and chunks past 128 rows.  Gradients are small
+    whole numbers, so every partial sum is exact and so is the result."""
+    import torch
+    from paper_2609_30379_amd import binding as B
+    r = np.random.default_rng(8)
+    ids = r.integers(-1, vocab, rows).astype(np.int32)
+    if vocab == 2:
+        ids[: rows - 5000] = 1                             # one run over nearly all chunks
+    dy = r.integers(-2, 3, (rows, 8)).astype(np.float32)
+    g = torch.full((vocab, 8), float("nan"), device="cuda")
+    B.nt_embedding_backward(torch.tensor(ids, device="cuda"), torch.tensor(dy, device="cuda"), g)
+    ok = ids >= 0
+    ref = np.stack([np.bincount(ids[ok], dy[ok, j].astype(np.float64), vocab) for j in range(8)], 1)
+    assert np.abs(ref).max() < 2 ** 24
+    assert np.array_equal(host(g), ref)
+
+
+def test_outputs_that_are_operands_are_refused():
+    import torch
+    from paper_2609_30379_amd import binding as B
+    t = torch.zeros((4, 8), device="cuda")
+    ids = torch.zeros(4, dtype=torch.int32, device="cuda")
+    with pytest.raises(B.NtError):
+        B.nt_embedding(t, ids, t)
+    with pytest.raises(B.NtError):
+        B.nt_embedding_backward(ids, t, t)
