@@ -29,7 +29,7 @@ struct WindowBwdParams {
   int64_t sum_q;
   int64_t items;
   bool narrow;
-  // gradients of the sinks from the queries past their window (window_sink_kernel)
+  // gradients of the sinks from the queries past their window (window_dkv_few_kernel<SINKS>, sink_sum_kernel)
   int split;                     // done apart, in pieces of `piece` rows
   int subs, pieces;              // blocks of 32 sinks, most pieces of a sample
   int64_t piece;                 // rows per piece
@@ -593,8 +593,7 @@ window_dkv_few_kernel(WindowBwdParams p) {
     rb = min((int64_t)n * p.group, ra + p.piece);
   } else {
     ra = (int64_t)ta * p.group;
-    rb = (int64_t)(jb >= p.sinks ? min(far, max(ta, window_end(je, p.left >= 0 ? p.left : n + m, off, n)))
-                   : p.split ? far : n) * p.group;
+    rb = (int64_t)(jb < p.sinks ? (p.split ? far : n) : p.left >= 0 ? max(ta, window_end(je, p.left, off, n)) : n) * p.group;
   }
   if (SINKS && ra >= rb) return;
   frag K[DP / 16], V[DP / 16];
@@ -698,9 +697,14 @@ sink_sum_kernel(WindowBwdParams p) {
 }
 
 // How the sinks' part past the window is cut: pieces of at least kSinkPiece rows,
-// fewer and longer ones where there are many blocks of sinks, so that the partial
-// sums stay bounded.
+// fewer and longer ones where there are many blocks of sinks.  The partial sums,
+// two of 32 keys each for dK and dV per block at least, may take 64 MB or as much
+// as q, k and v in fp32; where blocks of short samples or of many sinks would take
+// more, the keys' own workgroups walk all the rows.  (1100 samples of 40 tokens and
+// one of 20000, 4 sinks, 8 heads of 64: 553 us cut, 973 not; 1100 and one of 2000,
+// 341 and 335.)
 constexpr int kSinkPiece = 512, kSinkItems = 1024;
+constexpr int64_t kSinkFloats = 1 << 24;
 struct SinkPlan {
   int split, subs, pieces, dp;
   int64_t piece;
@@ -719,10 +723,12 @@ SinkPlan sink_plan(const nt_window_args& a) {
     const int64_t end = (m < 128 ? m : 128) - 1 + a.left - (m - n) + 1;
     rows = std::max(rows, (n - std::max<int64_t>(0, std::min(n, end))) * (a.heads / a.kv_heads));
   }
-  if (rows <= kSinkPiece) return s;
+  const int subs = (a.sinks + 31) / 32;
+  const int64_t blocks = (int64_t)Lq.batch * a.kv_heads * subs;
+  const int64_t operands = (Lq.sum_n * a.heads + 2 * Lk.sum_n * a.kv_heads) * a.head_dim;
+  if (rows <= kSinkPiece || blocks * 128 * s.dp > std::max(kSinkFloats, operands)) return s;
   s.split = 1;
-  s.subs = (a.sinks + 31) / 32;
-  const int64_t blocks = (int64_t)Lq.batch * a.kv_heads * s.subs;
+  s.subs = subs;
   const int64_t want = std::max<int64_t>(1, std::min(rows / kSinkPiece, kSinkItems / blocks));
   s.piece = ((rows + want - 1) / want + 127) / 128 * 128;
   s.pieces = (int)((rows + s.piece - 1) / s.piece);

@@ -313,3 +313,21 @@ def test_keys_without_any_query_get_zero_gradients():
     B.nt_window_attention_backward(ql, 2, 32, q, k, v, q.clone(), lse, q.clone(), q.clone(), dk, dv, kv_layout=kl, kv_heads=1,
                                    left=3, sinks=1)
     assert not bool(dk.any()) and not bool(dv.any())
+
+
+def test_outputs_that_are_one_another_are_refused():
+    import torch
+    from paper_2609_30379_amd import binding as B
+    lay = B.NestedLayout([3], cols=[1])
+    x = [torch.zeros((3, 8), device="cuda") for _ in range(7)]
+    q, k, v, o, do, g, h = x
+    lse = torch.zeros((1, 3), device="cuda")
+    for out in ((g, h, h), (g, g, h), (g, h, g)):
+        with pytest.raises(B.NtError, match="one another"):
+            B.nt_window_attention_backward(lay, 1, 8, q, k, v, o, lse, do, *out)
+
+
+def test_many_samples_one_long():
+    """More blocks of sinks than are handled apart: the keys' workgroups walk all rows."""
+    n = [3] * 1100 + [700]
+    run(n, n, 8, 8, 8, "f32", left=5, sinks=3)

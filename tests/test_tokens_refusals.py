@@ -136,6 +136,25 @@ def test_embedding_gradient_refusals(kw):
     assert embed_backward(**kw) == B.NT_ERR_INVALID_ARG and error()
 
 
+def test_embedding_outputs_that_are_operands():
+    assert embed() == B.NT_ERR_INVALID_ARG and "alias" in error()
+    assert embed_backward() == B.NT_ERR_INVALID_ARG and "alias" in error()
+    assert embed(c=1 << 25, ld_table=1 << 25, ld_y=1 << 25) == B.NT_ERR_OVERFLOW
+    assert embed_backward(c=1 << 25, ld=1 << 25, ld_dy=1 << 25) == B.NT_ERR_OVERFLOW
+
+
+def test_workspaces_stay_bounded():
+    """Many blocks of sinks, of which one long sample uses a few; tokens by the ten million."""
+    lengths = [40] * 499 + [20000]
+    a = window_args(q_layout=host(lengths), kv_layout=host(lengths), heads=8, kv_heads=8, head_dim=128, left=64, sinks=20000,
+                    ld_q=1024, ld_k=1024, ld_v=1024, ld_o=1024)
+    n = C.c_uint64()
+    assert status("nt_window_attention_backward_workspace", C.byref(a), C.byref(n)) == B.NT_OK
+    assert n.value < 1 << 30
+    assert status("nt_embedding_backward_workspace", 1 << 30, 1000, 512, C.byref(n)) == B.NT_OK
+    assert n.value < 18 << 30                              # 16 bytes a token, 65536 chunks of two partial rows
+
+
 def test_nothing_to_do_is_ok():
     assert embed(rows=0, ids=None, y=None) == B.NT_OK
     assert embed_backward(vocab=0, dtable=None) == B.NT_OK
