@@ -36,7 +36,10 @@ struct WindowParams {
 constexpr int kBlockShift = 7;                 // query rows per workgroup: 4 waves x 32
 
 constexpr int kFewShift = 5;                   // query rows per workgroup of the few-rows kernel
-constexpr int kFewBlocks = 128;                // at most so many blocks of 128 rows: blocks of 32 instead
+// At most so many blocks of 128 rows: blocks of 32 instead.  About 90 blocks (fp32,
+// 8 samples of 66 .. 317 tokens, 4 heads of 32): 8.4 us in blocks of 32, 21 in blocks
+// of 128; about 600 (bf16, 16 of 200 .. 1024, 8 heads of 64): 33 and 19.
+constexpr int kFewBlocks = 128;
 // Key tiles of a split, at least (few rows: eight per wave), and workgroups that a
 // call with few blocks is cut into: four per compute unit of few rows (64 tokens over
 // 500 .. 32000 keys, 8 key/value heads of 128: 816 us in 512, 769 in 1024, 796 in
@@ -99,7 +102,19 @@ __device__ __forceinline__ void write_out(const WindowParams& p, int64_t token, 
     p.lse[(int64_t)head * p.ld_lse + token] = l == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-
+// 128 rows per workgroup, 32 per wave, all four on the same tile of 64 keys (fp32:
+// 32), which lies in LDS twice: the next tile is stored while this one is read, one
+// barrier per tile.  Shared tiles quarter the reads of the keys, and S^T = K Q^T
+// needs only K from LDS, since Q stays in registers.  Bound by the products and the
+// exponentials together: of a wave's time the matrix cores take 38 .. 40 % and the
+// vector instructions as much (no LDS bank conflicts), which two or three waves per
+// SIMD overlap in part; a wave in its products goes first (s_setprio), so that the
+// others' exponentials fill the time around them (causal window to 8192, 128
+// channels: 265 us without, 255 with).  Tiles of 32 keys at 128 channels cost 14 %,
+// four waves per SIMD at 64 channels a third (spills).
+//   64 samples of about 230 tokens, 12 heads of 64, left = right = 64: 39 us, 2.5 TB/s
+//   4 samples to 8192, 16 heads on 4 of 128, causal window of 1024: 239 us, 716 TFLOP/s
+//   two chunks of 300 .. 700 tokens over 8000 .. 30000, 16 heads on 4 of 64: 102 us, 590
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, DP == 128 ? (sizeof(T) == 4 ? 1 : 2) : DP == 64 && sizeof(T) == 4 ? 2 : 3)
 window_rows_kernel(WindowParams p) {
@@ -273,7 +288,11 @@ window_rows_kernel(WindowParams p) {
 // tokens), its four waves on different key tiles, each with its own tile in LDS,
 // so no wave waits for another before the end, where the four running sums are
 // joined through LDS.  Bound by the cache's bytes: a wave keeps a whole tile in
-// flight while it works on the one before.
+// flight while it works on the one before, eight waves per compute unit together
+// 256 KB.  64 tokens over 500 .. 32000 keys, 32 heads on 8 of 128: 759 us, 5.0 TB/s
+// (a large copy reaches 4.7 here, a large read alone 4.0); one token over a window
+// of 1023 keys, 12 heads of 64: 10 us, the latency of four dependent tiles and the
+// launch.  Eight waves per workgroup: 9 us for that token, 794 .. 815 for the 64.
 template <typename T, int DP> struct FewShape {
   static constexpr int KT = sizeof(T) == 2 && DP < 128 ? 64 : 32;
   static constexpr int kTileBytes = KT * Tile<T, DP>::kLd * (int)sizeof(T);
@@ -416,7 +435,9 @@ window_few_kernel(WindowParams p) {
   }
 }
 
-// The splits' sums joined: four channels of a row per thread.
+// The splits' sums joined: o = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s, four
+// channels of a row per thread, the splits in order.  Bound by the partial outputs'
+// bytes: 8 us for the chunks above (26 MB written, read from the caches).
 template <typename T>
 __global__ void __launch_bounds__(256)
 window_join_kernel(WindowParams p) {

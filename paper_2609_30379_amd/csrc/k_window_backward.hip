@@ -36,7 +36,11 @@ struct WindowBwdParams {
   float *sink_part, *sink_sum;   // [batch][kv_heads][subs][pieces][2][32][DP], [batch][kv_heads][subs][2][32][DP]
 };
 
-// At most so many blocks of 128 rows, or of 128 keys, of all heads: blocks of 32 instead.
+// At most so many blocks of 128 rows, or of 128 keys, of all heads: blocks of 32
+// instead.  dQ: about 90 blocks (fp32, N 66 .. 317, 4 heads of 32) 12 us in blocks of
+// 32, 25 in blocks of 128; 600 (bf16, N 200 .. 1024, 8 heads on 2 of 64) 36 and 27.
+// dK, dV: 90 blocks 13 and 31; 170 (the bf16 ones) 28 and 54; 384 (N to 8192, 16 heads
+// on 4 of 128) 873 and 793.
 constexpr int kFewRowBlocks = 128, kFewKeyBlocks = 256;
 
 // First query past the window of the keys jb .. jl; the queries before it are
@@ -77,6 +81,13 @@ __device__ __forceinline__ void write_row(const WindowBwdParams& p, int64_t toke
   *reinterpret_cast<vec4*>((T*)p.dq + token * p.ld_dq + (int64_t)head * p.d + at) = w;
 }
 
+// dQ of 128 rows, 32 per wave: S^T = K Q^T, dP^T = V dO^T and dQ^T += K^T dS^T of one
+// tile of keys after another, the tiles twice in LDS as in the forward; dP starts from
+// -D, which saves the subtraction.  Q and dO stay in registers, so past 64 channels
+// tiles of 64 keys spill; of 32 they do not, and both K and V of the next tile can be
+// on their way at once (N to 8192, 16 heads on 4 of 128: 427 us in tiles of 64, 369 ..
+// 388 in tiles of 32, about 790 TFLOP/s).  Bound as the forward is: matrix cores 38 %,
+// vector instructions 27 % of the time.  64 channels, N 200 .. 1024: 27 us.
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, DP == 32 ? 3 : DP == 128 && sizeof(T) == 4 ? 1 : 2)
 window_dq_kernel(WindowBwdParams p) {
@@ -149,36 +160,36 @@ window_dq_kernel(WindowBwdParams p) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
       if (seen) {
-      read_part<DP, kG>(Ks, 32 * kb, 0, lane, X);
-      f32x16 S = f32x16{}, dP;
-      mask.hide(S, kb);
+        read_part<DP, kG>(Ks, 32 * kb, 0, lane, X);
+        f32x16 S = f32x16{}, dP;
+        mask.hide(S, kb);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) dP[e] = -delta;
-      if constexpr (NS > kG) {
-        read_part<DP, kG>(Ks, 32 * kb, kG, lane, Y);
-        S = product_part<kG>(X, Q, S);
-        read_part<DP, kG>(Vs, 32 * kb, 0, lane, X);
-        S = product_part<kG>(Y, Q + kG, S);
-        read_part<DP, kG>(Vs, 32 * kb, kG, lane, Y);
-        dP = product_part<kG>(X, G, dP);
-        read_across<DP>(Ks, 32 * kb, lane, tr, X);
-        dP = product_part<kG>(Y, G + kG, dP);
-      } else {
-        read_part<DP, kG>(Vs, 32 * kb, 0, lane, Y);
-        S = product_part<kG>(X, Q, S);
-        read_across<DP>(Ks, 32 * kb, lane, tr, X);
-        dP = product_part<kG>(Y, G, dP);
-      }
+        for (int e = 0; e < 16; ++e) dP[e] = -delta;
+        if constexpr (NS > kG) {
+          read_part<DP, kG>(Ks, 32 * kb, kG, lane, Y);
+          S = product_part<kG>(X, Q, S);
+          read_part<DP, kG>(Vs, 32 * kb, 0, lane, X);
+          S = product_part<kG>(Y, Q + kG, S);
+          read_part<DP, kG>(Vs, 32 * kb, kG, lane, Y);
+          dP = product_part<kG>(X, G, dP);
+          read_across<DP>(Ks, 32 * kb, lane, tr, X);
+          dP = product_part<kG>(Y, G + kG, dP);
+        } else {
+          read_part<DP, kG>(Vs, 32 * kb, 0, lane, Y);
+          S = product_part<kG>(X, Q, S);
+          read_across<DP>(Ks, 32 * kb, lane, tr, X);
+          dP = product_part<kG>(Y, G, dP);
+        }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) S[e] = __builtin_amdgcn_exp2f(fmaf(S[e], p.c, nlse2));
-      read_across<DP>(Ks, 32 * kb + 16, lane, tr, Y);
+        for (int e = 0; e < 16; ++e) S[e] = __builtin_amdgcn_exp2f(fmaf(S[e], p.c, nlse2));
+        read_across<DP>(Ks, 32 * kb + 16, lane, tr, Y);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) S[e] *= dP[e];
-      frag D;
-      to_operand(S, 0, D);
-      add_products(X, D, dQ);
-      to_operand(S, 1, D);
-      add_products(Y, D, dQ);
+        for (int e = 0; e < 16; ++e) S[e] *= dP[e];
+        frag D;
+        to_operand(S, 0, D);
+        add_products(X, D, dQ);
+        to_operand(S, 1, D);
+        add_products(Y, D, dQ);
       }
       if (kb == (KB - 1) / 2 && tile + 1 < kt.n) {
         stage.store(tid, Kb[1 - buf]);
@@ -199,7 +210,8 @@ window_dq_kernel(WindowBwdParams p) {
 
 // dQ of 32 rows per workgroup, its four waves on different key tiles, each with its
 // own tile in LDS, their sums joined in order at the end: for calls whose blocks of
-// 128 rows would leave most of the card idle.
+// 128 rows would leave most of the card idle.  Bound by latency: 12 us for fp32, N
+// 66 .. 317, 4 heads of 32 (25 in blocks of 128).
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, DP == 128 || (DP == 64 && sizeof(T) == 4) ? 1 : 2)
 window_dq_few_kernel(WindowBwdParams p) {
@@ -300,8 +312,9 @@ window_dq_few_kernel(WindowBwdParams p) {
 // One block of 32 rows (in LDS from row r0) against the wave's 32 keys, in steps of
 // at most four fragments: each step issues the reads of the next one before its
 // products, and the exponentials and score gradients run under products (the
-// compiler keeps to that order by itself here).  lse_s holds -lse log2(e) (-inf for a row past the end: weight 0), delta_s -D, pos_s the
-// rows' positions; a hidden pair's score starts from -inf.
+// compiler keeps to that order by itself here).  lse_s holds -lse log2(e) (-inf for a
+// row past the end: weight 0), delta_s -D, pos_s the rows' positions; a hidden pair's
+// score starts from -inf.
 template <typename T, int DP>
 __device__ __forceinline__ void key_block(const T* Qs, const T* Gs, const float* lse_s, const float* delta_s,
                                           const int* pos_s, int r0, bool cut_lo, bool cut_hi, int plo, int phi, float c,
@@ -329,13 +342,13 @@ __device__ __forceinline__ void key_block(const T* Qs, const T* Gs, const float*
   }
   if constexpr (NS > kG) {
     read_part<DP, kG>(Qs, r0, kG, lane, Y);
-      S = product_part<kG>(X, K, S);
-      read_part<DP, kG>(Gs, r0, 0, lane, X);
-      S = product_part<kG>(Y, K + kG, S);
-    } else {
+    S = product_part<kG>(X, K, S);
+    read_part<DP, kG>(Gs, r0, 0, lane, X);
+    S = product_part<kG>(Y, K + kG, S);
+  } else {
     read_part<DP, kG>(Gs, r0, 0, lane, Y);
-      S = product_part<kG>(X, K, S);
-  #pragma unroll
+    S = product_part<kG>(X, K, S);
+#pragma unroll
     for (int k = 0; k < kG; ++k) X[k] = Y[k];
   }
 #pragma unroll
@@ -346,12 +359,12 @@ __device__ __forceinline__ void key_block(const T* Qs, const T* Gs, const float*
   }
   if constexpr (NS > kG) {
     read_part<DP, kG>(Gs, r0, kG, lane, Y);
-      dP = product_part<kG>(X, V, dP);
-      read_across<DP>(Gs, r0, lane, tr, X);
-      dP = product_part<kG>(Y, V + kG, dP);
+    dP = product_part<kG>(X, V, dP);
+    read_across<DP>(Gs, r0, lane, tr, X);
+    dP = product_part<kG>(Y, V + kG, dP);
   } else {
     read_across<DP>(Gs, r0, lane, tr, Y);
-      dP = product_part<kG>(X, V, dP);
+    dP = product_part<kG>(X, V, dP);
 #pragma unroll
     for (int k = 0; k < ND; ++k) X[k] = Y[k];
   }
@@ -454,7 +467,15 @@ template <typename T, int DP, int RT, int THREADS> struct RowTile {
   }
 };
 
-// dK and dV of 128 keys, 32 per wave; the workgroup walks the rows that see them.
+// dK and dV of 128 keys, 32 per wave; the workgroup walks the rows that see them, 64
+// (fp32: 32) at a time through one tile of q and dout in LDS while the next is on its
+// way in registers.  K, V and both gradients of a wave's keys are 320 registers at 128
+// channels, so one wave per SIMD; two waves, forced, spill (1130 us for N to 8192, 16
+// heads on 4 of 128, against 761 .. 800), and dK and dV in workgroups of their own
+// compute S twice (907).  Bound by the products' latency with nothing else to issue:
+// matrix cores 33 % of the time it runs, 516 TFLOP/s, and 384 workgroups on 256
+// compute units take two turns.  Without any new rows to read it takes 9 % less;
+// workgroups that walk shared rows at the same time gain nothing.
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, DP == 128 || (DP == 64 && sizeof(T) == 4) ? 1 : 2)
 window_dkv_kernel(WindowBwdParams p) {
@@ -547,6 +568,9 @@ window_dkv_kernel(WindowBwdParams p) {
 //   all the later rows of the sample, which the workgroup of a block of keys would
 //   walk alone while the others have left.  A workgroup takes a piece of the rows
 //   (every row sees every sink there) and leaves its sums for sink_sum_kernel.
+// Bound by latency, four walks instead of one: 13 us for fp32, N 66 .. 317, 4 heads of
+// 32 (31 in blocks of 128 keys); 28 for N 200 .. 1024, 8 heads on 2 of 64 (54); the
+// sinks of N to 8192, 16 heads on 4 of 128: 22.
 template <typename T, int DP, bool SINKS>
 __global__ void __launch_bounds__(256, sizeof(T) == 4 || DP == 128 ? 1 : 2)
 window_dkv_few_kernel(WindowBwdParams p) {
@@ -673,7 +697,8 @@ window_dkv_few_kernel(WindowBwdParams p) {
   }
 }
 
-// The pieces' sums, added in order.
+// The pieces' sums, added in order, four channels per thread: 5 .. 7 us, the latency of
+// its loads.
 template <int DP>
 __global__ void __launch_bounds__(256)
 sink_sum_kernel(WindowBwdParams p) {
