@@ -33,6 +33,10 @@ struct WindowBwdParams {
   int split;                     // done apart, in pieces of `piece` rows
   int subs, pieces;              // blocks of 32 sinks, most pieces of a sample
   int64_t piece;                 // rows per piece
+  // the rows of a block of keys cut over workgroups
+  int parts;
+  float* key_part;               // [parts][2][sum M][kv_heads][d]
+  int64_t sum_k;
   float *sink_part, *sink_sum;   // [batch][kv_heads][subs][pieces][2][32][DP], [batch][kv_heads][subs][2][32][DP]
 };
 
@@ -471,10 +475,11 @@ template <typename T, int DP, int RT, int THREADS> struct RowTile {
 // (fp32: 32) at a time through one tile of q and dout in LDS while the next is on its
 // way in registers.  K, V and both gradients of a wave's keys are 320 registers at 128
 // channels, so one wave per SIMD; two waves, forced, spill (1130 us for N to 8192, 16
-// heads on 4 of 128, against 761 .. 800), and dK and dV in workgroups of their own
+// heads on 4 of 128, against 800), and dK and dV in workgroups of their own
 // compute S twice (907).  Bound by the products' latency with nothing else to issue:
-// matrix cores 33 % of the time it runs, 516 TFLOP/s, and 384 workgroups on 256
-// compute units take two turns.  Without any new rows to read it takes 9 % less;
+// matrix cores 33 % of the time it runs.  The 428 workgroups on 256 compute units
+// would take two turns, so their rows are cut in four parts: 761 .. 800 -> 679 us, 580
+// TFLOP/s, and 47 in the join.  Without any new rows to read it takes 9 % less;
 // workgroups that walk shared rows at the same time gain nothing.
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, DP == 128 || (DP == 64 && sizeof(T) == 4) ? 1 : 2)
@@ -489,8 +494,8 @@ window_dkv_kernel(WindowBwdParams p) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h32 = lane >> 5;
   const int64_t item = block_id();
   if (item >= p.items) return;
-  const int hk = (int)(item % p.kv_heads);
-  const int64_t b = item / p.kv_heads;
+  const int hk = (int)(item % p.kv_heads), part = p.parts > 1 ? (int)(item / p.kv_heads % p.parts) : 0;
+  const int64_t b = p.parts > 1 ? item / p.kv_heads / p.parts : item / p.kv_heads;
   const int i = find_sample(p.cu_k, p.batch, 1, kBlockShift, b, lane);
   const int q0 = p.cu_q[i], n = p.cu_q[i + 1] - q0, k0 = p.cu_k[i], m = p.cu_k[i + 1] - k0, off = m - n;
   const int64_t jb64 = (b - block_start(p.cu_k, i, 1, kBlockShift)) << kBlockShift;
@@ -514,16 +519,20 @@ window_dkv_kernel(WindowBwdParams p) {
   const int ta = p.right >= 0 ? min(max(0, jb - p.right - off), n) : 0;
   const int tb = max(ta, p.left >= 0 && (jb >= p.sinks || p.split) ? window_end(jl, p.left, off, n) : n);
   const int64_t rows = (int64_t)(tb - ta) * p.group;
-  const int tiles = (int)((rows + RT - 1) / RT);
+  int first = 0, tiles = (int)((rows + RT - 1) / RT);
+  if (p.parts > 1) {
+    first = (int)((int64_t)tiles * part / p.parts);
+    tiles = (int)((int64_t)tiles * (part + 1) / p.parts);
+  }
   RowTile<T, DP, RT, 256> in;
   // a tile's first row as (t0, g0), moved on by RT rows per tile
   const int step_t = RT / p.group, step_g = RT - step_t * p.group;
-  int t0 = ta, g0 = 0;
+  int t0 = ta + (int)((int64_t)first * RT / p.group), g0 = (int)((int64_t)first * RT % p.group);
   auto load = [&](int tile) {
     in.load(p, tid, hk, q0, t0, g0, min(tb - t0, RT + 1), (int)min((int64_t)RT, rows - (int64_t)tile * RT), off);
   };
-  if (tiles > 0) load(0);
-  for (int tile = 0; tile < tiles; ++tile) {
+  if (first < tiles) load(first);
+  for (int tile = first; tile < tiles; ++tile) {
     __syncthreads();
     in.store(tid, Qs, Gs, lse_s, delta_s, pos_s);
     __syncthreads();
@@ -543,7 +552,7 @@ window_dkv_kernel(WindowBwdParams p) {
       key_block<T, DP>(Qs, Gs, lse_s, delta_s, pos_s, r0, cut_lo, cut_hi, plo, phi, p.c, K, V, dK, dV, lane, tr);
   }
   if (!mine) return;
-  const bool more = p.split && j < p.sinks && tb < n;      // what the queries past the window add to a sink
+  const bool more = part == 0 && p.split && j < p.sinks && tb < n;      // what the queries past the window add to a sink
   const float* sum = p.sink_sum + (((int64_t)(i * p.kv_heads + hk) * p.subs + (j >> 5)) * 64 + (j & 31)) * DP;
 #pragma unroll
   for (int dt = 0; dt < ND; ++dt)
@@ -557,8 +566,35 @@ window_dkv_kernel(WindowBwdParams p) {
         a += *reinterpret_cast<const f32x4*>(sum + at);
         w += *reinterpret_cast<const f32x4*>(sum + 32 * DP + at);
       }
-      write_keys<T>(p, k0 + j, hk, at, a, w);
+      if (p.parts > 1) {
+        const int64_t width = (int64_t)p.kv_heads * p.d;
+        float* out = p.key_part + ((int64_t)part * 2 * p.sum_k + k0 + j) * width + (int64_t)hk * p.d + at;
+        *reinterpret_cast<f32x4*>(out) = a;
+        *reinterpret_cast<f32x4*>(out + p.sum_k * width) = w;
+      } else {
+        write_keys<T>(p, k0 + j, hk, at, a, w);
+      }
     }
+}
+
+// The parts' sums of dK and dV, added in order, four channels of a key per thread.
+// Bound by the partial sums' bytes: 219 MB for the four parts above, 47 us, 5.3 TB/s
+// with what is written.
+template <typename T>
+__global__ void __launch_bounds__(256)
+key_join_kernel(WindowBwdParams p) {
+  const int64_t blk = block_id();
+  if (blk >= p.items) return;
+  const int dv = p.kv_heads * (p.d / 4);
+  const int64_t u = blk * 256 + threadIdx.x, row = u / dv, plane = p.sum_k * dv * 4;
+  if (row >= p.sum_k) return;
+  const int c = (int)(u - row * dv) * 4, hk = c / p.d;
+  f32x4 a = {0.f, 0.f, 0.f, 0.f}, w = a;
+  for (int x = 0; x < p.parts; ++x) {
+    a += *reinterpret_cast<const f32x4*>(p.key_part + 2 * x * plane + u * 4);
+    w += *reinterpret_cast<const f32x4*>(p.key_part + (2 * x + 1) * plane + u * 4);
+  }
+  write_keys<T>(p, row, hk, c - hk * p.d, a, w);
 }
 
 // dK and dV of 32 keys per workgroup, its four waves on different tiles of rows,
@@ -730,16 +766,55 @@ sink_sum_kernel(WindowBwdParams p) {
 // 341 and 335.)
 constexpr int kSinkPiece = 512, kSinkItems = 1024;
 constexpr int64_t kSinkFloats = 1 << 24;
-struct SinkPlan {
+struct BackwardPlan {
+  bool few_q, few_k;
+  int parts;
   int split, subs, pieces, dp;
   int64_t piece;
-  size_t delta_bytes, part_bytes, sum_bytes;
+  size_t delta_bytes, part_bytes, sum_bytes, key_bytes;
 };
-SinkPlan sink_plan(const nt_window_args& a) {
-  SinkPlan s{};
+
+// Parts that the rows of a block of keys are cut into, where the blocks take few turns
+// on the compute units and the last turn leaves many idle: a part keeps at least
+// kPartRows rows, and each step up has to save a tenth of the turns.  Whole backward,
+// uncut and cut: N 8192 and 4500, window 2048, 16 heads on 4 of 128 (400 blocks on 256
+// places, 3 parts) 1070 and 961 us; N 9000 causal, 32 heads on 4 of 128 (284, 3 parts)
+// 4037 and 2950; three of 4000, fp32, 16 heads on 4 of 64 (384, 2 parts) 7249 and 6048.
+// Where the turns are even, four parts all the same: 8192 causal, 16 heads on 8 of 128
+// (512 blocks) 1230 and 1347; four of 2048, every key (512) 587 and 700.
+constexpr int kPartRows = 1024, kMostParts = 4;
+int key_parts(const nt_window_args& a, int64_t blocks, int dp) {
+  // workgroups that are resident, by registers
+  const int64_t slots = 256 * (dp == 128 || (dp == 64 && a.dtype == NT_F32) ? 1 : dp == 64 ? 2 : 3);
+  int64_t rows = 0;                                        // that a block of keys is seen by
+  for (int32_t n : a.q_layout->lengths) rows = std::max<int64_t>(rows, n);
+  if (a.left >= 0 && a.right >= 0) rows = std::min<int64_t>(rows, (int64_t)a.left + a.right + 128);
+  rows *= a.heads / a.kv_heads;
+  int best = 1;
+  double turns = (double)((blocks + slots - 1) / slots);
+  for (int x = 2; x <= kMostParts && rows / x >= kPartRows; ++x) {
+    const double t = (double)((blocks * x + slots - 1) / slots) / x;
+    if (t < 0.9 * turns) best = x, turns = t;
+  }
+  return best;
+}
+
+BackwardPlan backward_plan(const nt_window_args& a) {
+  BackwardPlan s{};
   const nt_layout &Lq = *a.q_layout, &Lk = *a.kv_layout;
   s.delta_bytes = ((size_t)a.heads * Lq.sum_n * sizeof(float) + 15) / 16 * 16;
   s.dp = a.head_dim <= 32 ? 32 : a.head_dim <= 64 ? 64 : 128;
+  // blocks of 128 rows or keys, or of 32 where those would leave most of the card idle
+  auto blocks_of = [&](const nt_layout& L, int mul) {
+    int64_t n = 0;
+    for (int32_t x : L.lengths) n += ((int64_t)x * mul + 127) >> 7;
+    return n * a.kv_heads;
+  };
+  const int64_t key_blocks = blocks_of(Lk, 1);
+  s.few_q = blocks_of(Lq, a.heads / a.kv_heads) <= kFewRowBlocks;
+  s.few_k = key_blocks <= kFewKeyBlocks;
+  s.parts = s.few_k ? 1 : key_parts(a, key_blocks, s.dp);
+  if (s.parts > 1) s.key_bytes = (size_t)s.parts * 2 * Lk.sum_n * a.kv_heads * a.head_dim * sizeof(float);
   if (a.left < 0 || a.sinks == 0) return s;
   int64_t rows = 0;                                        // most rows past the window of the first keys
   for (int i = 0; i < Lq.batch; ++i) {
@@ -763,20 +838,14 @@ SinkPlan sink_plan(const nt_window_args& a) {
 }
 
 template <typename T, int DP>
-hipError_t launch_backward(WindowBwdParams p, const nt_layout& Lq, const nt_layout& Lk, hipStream_t s) {
-  // blocks of 128 rows or keys, or of 32 where those would leave most of the card idle
-  auto blocks = [&](const nt_layout& L, int mul) {
-    int64_t n = 0;
-    for (int32_t x : L.lengths) n += ((int64_t)x * mul + 127) >> 7;
-    return n * p.kv_heads;
-  };
+hipError_t launch_backward(WindowBwdParams p, const BackwardPlan& w, const nt_layout& Lq, const nt_layout& Lk,
+                           hipStream_t s) {
   auto items = [&](const nt_layout& L, int mul, int shift) {
     return L.sum_n ? block_count(L.sum_n, L.batch, mul, shift) * p.kv_heads : 0;
   };
-  const bool few_q = blocks(Lq, p.group) <= kFewRowBlocks, few_k = blocks(Lk, 1) <= kFewKeyBlocks;
-  p.items = items(Lq, p.group, few_q ? kFewShift : kBlockShift);
+  p.items = items(Lq, p.group, w.few_q ? kFewShift : kBlockShift);
   if (p.items > 0) {
-    if (few_q) window_dq_few_kernel<T, DP><<<folded_grid(p.items), 256, 0, s>>>(p);
+    if (w.few_q) window_dq_few_kernel<T, DP><<<folded_grid(p.items), 256, 0, s>>>(p);
     else window_dq_kernel<T, DP><<<folded_grid(p.items), 256, 0, s>>>(p);
   }
   if (hipError_t e = hipGetLastError()) return e;
@@ -788,10 +857,15 @@ hipError_t launch_backward(WindowBwdParams p, const nt_layout& Lq, const nt_layo
     sink_sum_kernel<DP><<<folded_grid(p.items), 256, 0, s>>>(p);
     if (hipError_t e = hipGetLastError()) return e;
   }
-  p.items = items(Lk, 1, few_k ? kFewShift : kBlockShift);
+  p.items = items(Lk, 1, w.few_k ? kFewShift : kBlockShift) * p.parts;
   if (p.items > 0) {
-    if (few_k) window_dkv_few_kernel<T, DP, false><<<folded_grid(p.items), 256, 0, s>>>(p);
+    if (w.few_k) window_dkv_few_kernel<T, DP, false><<<folded_grid(p.items), 256, 0, s>>>(p);
     else window_dkv_kernel<T, DP><<<folded_grid(p.items), 256, 0, s>>>(p);
+  }
+  if (hipError_t e = hipGetLastError()) return e;
+  if (p.parts > 1) {
+    p.items = (p.sum_k * p.kv_heads * (p.d / 4) + 255) / 256;
+    key_join_kernel<T><<<folded_grid(p.items), 256, 0, s>>>(p);
   }
   return hipGetLastError();
 }
@@ -799,8 +873,8 @@ hipError_t launch_backward(WindowBwdParams p, const nt_layout& Lq, const nt_layo
 }  // namespace
 
 size_t window_backward_workspace_bytes(const nt_window_args& a) {
-  const SinkPlan s = sink_plan(a);
-  return s.delta_bytes + s.part_bytes + s.sum_bytes;
+  const BackwardPlan s = backward_plan(a);
+  return s.delta_bytes + s.part_bytes + s.sum_bytes + s.key_bytes;
 }
 
 hipError_t launch_window_backward(const nt_window_args& a, hipStream_t s) {
@@ -827,20 +901,23 @@ hipError_t launch_window_backward(const nt_window_args& a, hipStream_t s) {
   p.lse = a.lse;
   p.delta = (float*)a.workspace;
   p.sum_q = Lq.sum_n;
-  const SinkPlan sp = sink_plan(a);
+  const BackwardPlan sp = backward_plan(a);
+  p.parts = sp.parts;
+  p.sum_k = Lk.sum_n;
   p.split = sp.split;
   p.subs = sp.subs;
   p.pieces = sp.pieces;
   p.piece = sp.piece;
   p.sink_part = (float*)((char*)a.workspace + sp.delta_bytes);
   p.sink_sum = (float*)((char*)a.workspace + sp.delta_bytes + sp.part_bytes);
+  p.key_part = (float*)((char*)a.workspace + sp.delta_bytes + sp.part_bytes + sp.sum_bytes);
   const bool bf = a.dtype == NT_BF16;
   const int size = bf ? 2 : 4;
   p.narrow = win::narrow_stride(a.ld_q, size) && win::narrow_stride(a.ld_dout, size) &&
              win::narrow_stride(a.ld_k, size) && win::narrow_stride(a.ld_v, size);
-  if (p.d <= 32) return bf ? launch_backward<bf16, 32>(p, Lq, Lk, s) : launch_backward<float, 32>(p, Lq, Lk, s);
-  if (p.d <= 64) return bf ? launch_backward<bf16, 64>(p, Lq, Lk, s) : launch_backward<float, 64>(p, Lq, Lk, s);
-  return bf ? launch_backward<bf16, 128>(p, Lq, Lk, s) : launch_backward<float, 128>(p, Lq, Lk, s);
+  if (p.d <= 32) return bf ? launch_backward<bf16, 32>(p, sp, Lq, Lk, s) : launch_backward<float, 32>(p, sp, Lq, Lk, s);
+  if (p.d <= 64) return bf ? launch_backward<bf16, 64>(p, sp, Lq, Lk, s) : launch_backward<float, 64>(p, sp, Lq, Lk, s);
+  return bf ? launch_backward<bf16, 128>(p, sp, Lq, Lk, s) : launch_backward<float, 128>(p, sp, Lq, Lk, s);
 }
 
 }  // namespace nt

@@ -331,3 +331,9 @@ def test_many_samples_one_long():
     """More blocks of sinks than are handled apart: the keys' workgroups walk all rows."""
     n = [3] * 1100 + [700]
     run(n, n, 8, 8, 8, "f32", left=5, sinks=3)
+
+
+@pytest.mark.parametrize("dtype,left,right,sinks", [("bf16", -1, 0, 0), ("f32", 500, 400, 4)])
+def test_rows_of_keys_in_parts(dtype, left, right, sinks):
+    """320 blocks of keys on 256 places: their rows are cut in two and the sums joined."""
+    run([1100, 40], [1100, 40], 64, 32, 72, dtype, left, right, sinks)
