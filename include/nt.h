@@ -709,7 +709,8 @@ typedef struct {
  * or too small workspace),
  * NT_ERR_LAYOUT_MISMATCH (batch sizes differ), NT_ERR_UNSUPPORTED (head_dim, more
  * than 65536 heads),
- * NT_ERR_OVERFLOW (a sample of 2^30 tokens or more), NT_ERR_HIP.             */
+ * NT_ERR_OVERFLOW (a sample of 2^30 tokens or more, heads times tokens beyond the
+ * launch limit), NT_ERR_HIP.                                                 */
 nt_status nt_window_attention(const nt_window_args* args, void* stream);
 nt_status nt_window_attention_workspace(const nt_window_args* args, uint64_t* bytes);
 
