@@ -40,13 +40,16 @@ constexpr int kFewShift = 5;                   // query rows per workgroup of th
 // 8 samples of 66 .. 317 tokens, 4 heads of 32): 8.4 us in blocks of 32, 21 in blocks
 // of 128; about 600 (bf16, 16 of 200 .. 1024, 8 heads of 64): 33 and 19.
 constexpr int kFewBlocks = 128;
-// Key tiles of a split, at least (few rows: eight per wave), and workgroups that a
+// Key tiles of a split, at least: eight per wave of few rows, two of fp32 past 64
+// channels, whose products take 5 us a tile (3 tokens over 366 .. 733 keys, 16 heads on
+// 2 of 128: 34 us in splits of 32 tiles, 29 of 16, 20 of 8; 28 samples of 46 over to
+// 503 keys, 3 heads of 64: 17 of 32, 20 of 8).  And workgroups that a
 // call with few blocks is cut into: four per compute unit of few rows (64 tokens over
 // 500 .. 32000 keys, 8 key/value heads of 128: 816 us in 512, 769 in 1024, 796 in
 // 2048), else as many as are resident, three up to 64 channels (chunks of 300 .. 700
 // tokens over 8000 .. 30000, 16 heads of 64: 135 us in 512, 114 in 768, 122 in 1024)
 // and two past that.
-constexpr int kFewChunk = 32, kRowsChunk = 8, kFewItems = 1024, kRowsItems = 256;
+constexpr int kFewChunk = 32, kFewChunkWide = 8, kRowsChunk = 8, kFewItems = 1024, kRowsItems = 256;
 
 // One tile of KB x 32 keys against the wave's 32 rows: scores S become weights, O
 // and l are brought to the maximum in use.
@@ -502,12 +505,13 @@ WindowPlan window_plan(const nt_window_args& a) {
   // leave most of the card idle.
   w.few = most_rows <= 32 || blocks * a.kv_heads <= kFewBlocks;
   const int shift = w.few ? kFewShift : kBlockShift;
-  const int kt = a.dtype == NT_BF16 && !(w.few && a.head_dim > 64) ? 64 : 32;
+  const bool bf = a.dtype == NT_BF16;
+  const int kt = bf && !(w.few && a.head_dim > 64) ? 64 : 32;
   w.blocks = win::block_count(Lq.sum_n, Lq.batch, G, shift);
   int64_t total, most;
   count_tiles(a, shift, kt, &total, &most);
   const int items = w.few ? kFewItems : kRowsItems * (a.head_dim <= 64 ? 3 : 2);
-  w.chunk = (int)std::max<int64_t>(w.few ? kFewChunk : kRowsChunk, (total + items - 1) / items);
+  w.chunk = (int)std::max<int64_t>(w.few ? (!bf && a.head_dim > 64 ? kFewChunkWide : kFewChunk) : kRowsChunk, (total + items - 1) / items);
   // every block gets the splits of the longest one, most of them empty where lengths
   // differ much: bounded, so that empty workgroups never outweigh the work
   const int64_t room = std::max<int64_t>(1, 16 * (int64_t)items / std::max<int64_t>(1, w.blocks * a.kv_heads));

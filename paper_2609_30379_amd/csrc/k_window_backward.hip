@@ -436,6 +436,15 @@ __device__ __forceinline__ void write_keys(const WindowBwdParams& p, int64_t row
   *reinterpret_cast<vec4*>((T*)p.dv + row * p.ld_dv + (int64_t)hk * p.d + at) = w;
 }
 
+// The same of one part of the rows, for key_join_kernel.
+__device__ __forceinline__ void write_part(const WindowBwdParams& p, int part, int64_t row, int hk, int at,
+                                           const f32x4& dk, const f32x4& dv) {
+  const int64_t width = (int64_t)p.kv_heads * p.d;
+  float* out = p.key_part + ((int64_t)part * 2 * p.sum_k + row) * width + (int64_t)hk * p.d + at;
+  *reinterpret_cast<f32x4*>(out) = dk;
+  *reinterpret_cast<f32x4*>(out + p.sum_k * width) = dv;
+}
+
 // The rows of a tile on their way into LDS: q and dout of all query heads that
 // share the keys, and the rows' statistics.  THREADS threads of index tid.
 template <typename T, int DP, int RT, int THREADS> struct RowTile {
@@ -567,10 +576,7 @@ window_dkv_kernel(WindowBwdParams p) {
         w += *reinterpret_cast<const f32x4*>(sum + 32 * DP + at);
       }
       if (p.parts > 1) {
-        const int64_t width = (int64_t)p.kv_heads * p.d;
-        float* out = p.key_part + ((int64_t)part * 2 * p.sum_k + k0 + j) * width + (int64_t)hk * p.d + at;
-        *reinterpret_cast<f32x4*>(out) = a;
-        *reinterpret_cast<f32x4*>(out + p.sum_k * width) = w;
+        write_part(p, part, k0 + j, hk, at, a, w);
       } else {
         write_keys<T>(p, k0 + j, hk, at, a, w);
       }
@@ -626,14 +632,15 @@ window_dkv_few_kernel(WindowBwdParams p) {
   const int64_t item = block_id();
   if (item >= p.items) return;
   const int hk = (int)(item % p.kv_heads);
-  int i, sub = 0, piece = 0, jb;
+  int i, sub = 0, piece = 0, part = 0, jb;
   if (SINKS) {
     piece = (int)(item / p.kv_heads % p.pieces);
     sub = (int)(item / p.kv_heads / p.pieces % p.subs);
     i = (int)(item / p.kv_heads / p.pieces / p.subs);
     jb = 32 * sub;
   } else {
-    const int64_t b = item / p.kv_heads;
+    part = p.parts > 1 ? (int)(item / p.kv_heads % p.parts) : 0;
+    const int64_t b = p.parts > 1 ? item / p.kv_heads / p.parts : item / p.kv_heads;
     i = find_sample(p.cu_k, p.batch, 1, kFewShift, b, lane);
     jb = (int)((b - block_start(p.cu_k, i, 1, kFewShift)) << kFewShift);
   }
@@ -654,6 +661,11 @@ window_dkv_few_kernel(WindowBwdParams p) {
   } else {
     ra = (int64_t)ta * p.group;
     rb = (int64_t)(jb < p.sinks ? (p.split ? far : n) : p.left >= 0 ? max(ta, window_end(je, p.left, off, n)) : n) * p.group;
+    if (p.parts > 1) {
+      const int64_t tiles = max((int64_t)0, rb - ra + RT - 1) / RT, end = ra + tiles * (part + 1) / p.parts * RT;
+      ra += tiles * part / p.parts * RT;
+      rb = min(rb, end);
+    }
   }
   if (SINKS && ra >= rb) return;
   frag K[DP / 16], V[DP / 16];
@@ -723,12 +735,13 @@ window_dkv_few_kernel(WindowBwdParams p) {
       *reinterpret_cast<f32x4*>(out + key * DP + at) = total[0][u];
       *reinterpret_cast<f32x4*>(out + (32 + key) * DP + at) = total[1][u];
     } else if (jb + key < m && at < p.d) {
-      if (p.split && jb + key < p.sinks && far < n) {
+      if (part == 0 && p.split && jb + key < p.sinks && far < n) {
         const float* sum = p.sink_sum + (((int64_t)(i * p.kv_heads + hk) * p.subs + (jb >> 5)) * 64 + key) * DP + at;
         total[0][u] += *reinterpret_cast<const f32x4*>(sum);
         total[1][u] += *reinterpret_cast<const f32x4*>(sum + 32 * DP);
       }
-      write_keys<T>(p, k0 + jb + key, hk, at, total[0][u], total[1][u]);
+      if (p.parts > 1) write_part(p, part, k0 + jb + key, hk, at, total[0][u], total[1][u]);
+      else write_keys<T>(p, k0 + jb + key, hk, at, total[0][u], total[1][u]);
     }
   }
 }
@@ -757,14 +770,17 @@ sink_sum_kernel(WindowBwdParams p) {
   if (pieces > 0) *reinterpret_cast<f32x4*>(p.sink_sum + blk * 64 * DP + part * 1024 + threadIdx.x * 4) = a;
 }
 
-// How the sinks' part past the window is cut: pieces of at least kSinkPiece rows,
+// How the sinks' part past the window is cut: pieces of at least kSinkCut rows,
 // fewer and longer ones where there are many blocks of sinks.  The partial sums,
 // two of 32 keys each for dK and dV per block at least, may take 64 MB or as much
 // as q, k and v in fp32; where blocks of short samples or of many sinks would take
 // more, the keys' own workgroups walk all the rows.  (1100 samples of 40 tokens and
 // one of 20000, 4 sinks, 8 heads of 64: 553 us cut, 973 not; 1100 and one of 2000,
 // 341 and 335.)
-constexpr int kSinkPiece = 512, kSinkItems = 1024;
+// Pieces of kSinkCut rows, for more than kSinkPiece rows (fp32, 2 samples of 463, 3
+// heads on 1 of 128, window of 110 to both sides: 190 us in pieces of 512 and uncut
+// parts, 137 with both).
+constexpr int kSinkPiece = 512, kSinkCut = 256, kSinkItems = 1024;
 constexpr int64_t kSinkFloats = 1 << 24;
 struct BackwardPlan {
   bool few_q, few_k;
@@ -782,14 +798,17 @@ struct BackwardPlan {
 // 4037 and 2950; three of 4000, fp32, 16 heads on 4 of 64 (384, 2 parts) 7249 and 6048.
 // Where the turns are even, four parts all the same: 8192 causal, 16 heads on 8 of 128
 // (512 blocks) 1230 and 1347; four of 2048, every key (512) 587 and 700.
-constexpr int kPartRows = 1024, kMostParts = 4;
-int key_parts(const nt_window_args& a, int64_t blocks, int dp) {
+// Blocks of 32 keys are cut where they leave room, in parts of kFewPartRows: the join's
+// launch has to pay (fp32, N 66 .. 317, 4 heads of 32, parts of 256: 34 and 40 us).
+constexpr int kPartRows = 1024, kMostParts = 4, kFewPartRows = 512, kMostFewParts = 8;
+int key_parts(const nt_window_args& a, int64_t blocks, bool few, int dp) {
   // workgroups that are resident, by registers
   const int64_t slots = 256 * (dp == 128 || (dp == 64 && a.dtype == NT_F32) ? 1 : dp == 64 ? 2 : 3);
   int64_t rows = 0;                                        // that a block of keys is seen by
   for (int32_t n : a.q_layout->lengths) rows = std::max<int64_t>(rows, n);
   if (a.left >= 0 && a.right >= 0) rows = std::min<int64_t>(rows, (int64_t)a.left + a.right + 128);
   rows *= a.heads / a.kv_heads;
+  if (few) return (int)std::max<int64_t>(1, std::min({slots / std::max<int64_t>(1, blocks), rows / kFewPartRows, (int64_t)kMostFewParts}));
   int best = 1;
   double turns = (double)((blocks + slots - 1) / slots);
   for (int x = 2; x <= kMostParts && rows / x >= kPartRows; ++x) {
@@ -805,15 +824,14 @@ BackwardPlan backward_plan(const nt_window_args& a) {
   s.delta_bytes = ((size_t)a.heads * Lq.sum_n * sizeof(float) + 15) / 16 * 16;
   s.dp = a.head_dim <= 32 ? 32 : a.head_dim <= 64 ? 64 : 128;
   // blocks of 128 rows or keys, or of 32 where those would leave most of the card idle
-  auto blocks_of = [&](const nt_layout& L, int mul) {
+  auto blocks_of = [&](const nt_layout& L, int mul, int shift) {
     int64_t n = 0;
-    for (int32_t x : L.lengths) n += ((int64_t)x * mul + 127) >> 7;
+    for (int32_t x : L.lengths) n += ((int64_t)x * mul + (1 << shift) - 1) >> shift;
     return n * a.kv_heads;
   };
-  const int64_t key_blocks = blocks_of(Lk, 1);
-  s.few_q = blocks_of(Lq, a.heads / a.kv_heads) <= kFewRowBlocks;
-  s.few_k = key_blocks <= kFewKeyBlocks;
-  s.parts = s.few_k ? 1 : key_parts(a, key_blocks, s.dp);
+  s.few_q = blocks_of(Lq, a.heads / a.kv_heads, kBlockShift) <= kFewRowBlocks;
+  s.few_k = blocks_of(Lk, 1, kBlockShift) <= kFewKeyBlocks;
+  s.parts = key_parts(a, blocks_of(Lk, 1, s.few_k ? kFewShift : kBlockShift), s.few_k, s.dp);
   if (s.parts > 1) s.key_bytes = (size_t)s.parts * 2 * Lk.sum_n * a.kv_heads * a.head_dim * sizeof(float);
   if (a.left < 0 || a.sinks == 0) return s;
   int64_t rows = 0;                                        // most rows past the window of the first keys
@@ -829,7 +847,7 @@ BackwardPlan backward_plan(const nt_window_args& a) {
   if (rows <= kSinkPiece || blocks * 128 * s.dp > std::max(kSinkFloats, operands)) return s;
   s.split = 1;
   s.subs = subs;
-  const int64_t want = std::max<int64_t>(1, std::min(rows / kSinkPiece, kSinkItems / blocks));
+  const int64_t want = std::max<int64_t>(1, std::min(rows / kSinkCut, kSinkItems / blocks));
   s.piece = ((rows + want - 1) / want + 127) / 128 * 128;
   s.pieces = (int)((rows + s.piece - 1) / s.piece);
   s.part_bytes = (size_t)blocks * s.pieces * 64 * s.dp * sizeof(float);

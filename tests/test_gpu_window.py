@@ -337,3 +337,14 @@ def test_many_samples_one_long():
 def test_rows_of_keys_in_parts(dtype, left, right, sinks):
     """320 blocks of keys on 256 places: their rows are cut in two and the sums joined."""
     run([1100, 40], [1100, 40], 64, 32, 72, dtype, left, right, sinks)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_of_few_keys_in_parts(dtype):
+    """Blocks of 32 keys that leave places free, groups that end inside a part."""
+    run([401, 5], [401, 5], 3, 1, 96, dtype, 110, 110, 4)
+    run([300], [350], 5, 1, 24, dtype)
+
+
+def test_a_token_over_wide_fp32_keys():
+    run([1, 2, 1], [733, 300, 0], 8, 1, 128, "f32", left=500, sinks=4, train=False)
