@@ -770,18 +770,20 @@ sink_sum_kernel(WindowBwdParams p) {
   if (pieces > 0) *reinterpret_cast<f32x4*>(p.sink_sum + blk * 64 * DP + part * 1024 + threadIdx.x * 4) = a;
 }
 
-// How the sinks' part past the window is cut: pieces of at least kSinkCut rows,
-// fewer and longer ones where there are many blocks of sinks.  The partial sums,
-// two of 32 keys each for dK and dV per block at least, may take 64 MB or as much
-// as q, k and v in fp32; where blocks of short samples or of many sinks would take
-// more, the keys' own workgroups walk all the rows.  (1100 samples of 40 tokens and
-// one of 20000, 4 sinks, 8 heads of 64: 553 us cut, 973 not; 1100 and one of 2000,
-// 341 and 335.)
-// Pieces of kSinkCut rows, for more than kSinkPiece rows (fp32, 2 samples of 463, 3
-// heads on 1 of 128, window of 110 to both sides: 190 us in pieces of 512 and uncut
-// parts, 137 with both).
+// How the sinks' part past the window is cut: pieces of at least kSinkPiece rows, or
+// kSinkCut where those would leave compute units idle, fewer and longer ones where
+// there are many blocks of sinks.  (N to 8192, 16 heads on 4 of 128, pieces of 512 and
+// 256: 22 and 29 us; N 200 .. 1024, 8 on 2 of 64: 10 and 8; the backward of fp32, 2
+// samples of 463, 3 heads on 1 of 128, window of 110 to both sides: 190 us in pieces of
+// 512 and uncut parts, 137 with both.)
+// The partial sums, two of 32 keys each for dK and dV per block at least, may take 64
+// MB or as much as q, k and v in fp32; where blocks of short samples or of many sinks
+// would take more, the keys' own workgroups walk all the rows.  (1100 samples of 40
+// tokens and one of 20000, 4 sinks, 8 heads of 64: 553 us cut, 973 not; 1100 and one of
+// 2000, 341 and 335.)
 constexpr int kSinkPiece = 512, kSinkCut = 256, kSinkItems = 1024;
 constexpr int64_t kSinkFloats = 1 << 24;
+
 struct BackwardPlan {
   bool few_q, few_k;
   int parts;
@@ -847,7 +849,8 @@ BackwardPlan backward_plan(const nt_window_args& a) {
   if (rows <= kSinkPiece || blocks * 128 * s.dp > std::max(kSinkFloats, operands)) return s;
   s.split = 1;
   s.subs = subs;
-  const int64_t want = std::max<int64_t>(1, std::min(rows / kSinkCut, kSinkItems / blocks));
+  const int64_t cut = blocks * (rows / kSinkPiece) < 256 ? kSinkCut : kSinkPiece;
+  const int64_t want = std::max<int64_t>(1, std::min(rows / cut, kSinkItems / blocks));
   s.piece = ((rows + want - 1) / want + 127) / 128 * 128;
   s.pieces = (int)((rows + s.piece - 1) / s.piece);
   s.part_bytes = (size_t)blocks * s.pieces * 64 * s.dp * sizeof(float);
