@@ -830,7 +830,9 @@ nt_status on_current_device(const nt_layout* L) {
   return NT_OK;
 }
 
-nt_status window_operands(const nt_window_args& a) {
+// Pointers, strides and the layouts' device of a window attention call, in that
+// order: what the arguments alone show is reported wherever the layouts live.
+nt_status window_operands(const nt_window_args& a, bool backward) {
   const int ve = vec_elems(a.dtype);
   const int64_t cq = (int64_t)a.heads * a.head_dim, ck = (int64_t)a.kv_heads * a.head_dim;
   const int64_t nq = a.q_layout->sum_n, nk = a.kv_layout->sum_n;
@@ -843,6 +845,20 @@ nt_status window_operands(const nt_window_args& a) {
     return nt::fail(NT_ERR_INVALID_ARG, "o must not alias q, k or v");
   if (a.lse && ((reinterpret_cast<uintptr_t>(a.lse) & 3u) || a.ld_lse < nq))
     return nt::fail(NT_ERR_INVALID_ARG, "lse must be 4-byte aligned with ld_lse >= the query rows");
+  if (backward) {
+    if (nq > 0 && !a.lse) return nt::fail(NT_ERR_INVALID_ARG, "the backward needs the forward's lse");
+    if (nt_status st = matrix_operand(a.dout, a.ld_dout, cq, nq, ve, "dout")) return st;
+    if (nt_status st = matrix_operand(a.dq, a.ld_dq, cq, nq, ve, "dq")) return st;
+    if (nt_status st = matrix_operand(a.dk, a.ld_dk, ck, nk, ve, "dk")) return st;
+    if (nt_status st = matrix_operand(a.dv, a.ld_dv, ck, nk, ve, "dv")) return st;
+    for (const void* out : {(const void*)(nq ? a.dq : nullptr), (const void*)(nk ? a.dk : nullptr), (const void*)(nk ? a.dv : nullptr)})
+      if (out && (out == a.q || out == a.k || out == a.v || out == a.o || out == a.dout))
+        return nt::fail(NT_ERR_INVALID_ARG, "dq, dk and dv must not alias the operands");
+    if ((nk && a.dk == a.dv) || (nq && nk && (a.dq == a.dk || a.dq == a.dv)))
+      return nt::fail(NT_ERR_INVALID_ARG, "dq, dk and dv must not alias one another");
+  } else if (a.kv_lengths && (reinterpret_cast<uintptr_t>(a.kv_lengths) & 3u)) {
+    return nt::fail(NT_ERR_INVALID_ARG, "kv_lengths must be 4-byte aligned");
+  }
   if (nt_status st = on_current_device(a.q_layout)) return st;
   return on_current_device(a.kv_layout);
 }
@@ -876,9 +892,7 @@ nt_status nt_window_attention(const nt_window_args* args, void* stream) {
   g_last_error.clear();
   nt_window_args a;
   if (nt_status st = window_sizes(args, &a)) return st;
-  if (nt_status st = window_operands(a)) return st;
-  if (a.kv_lengths && (reinterpret_cast<uintptr_t>(a.kv_lengths) & 3u))
-    return nt::fail(NT_ERR_INVALID_ARG, "kv_lengths must be 4-byte aligned");
+  if (nt_status st = window_operands(a, false)) return st;
   if (a.q_layout->sum_n == 0) return NT_OK;
   if (nt_status st = need_workspace(nt::window_workspace_bytes(a), a.workspace, a.workspace_bytes,
                                     "nt_window_attention_workspace"))
@@ -900,21 +914,8 @@ nt_status nt_window_attention_backward(const nt_window_args* args, void* stream)
   nt_window_args a;
   if (nt_status st = window_sizes(args, &a)) return st;
   if (a.kv_lengths) return nt::fail(NT_ERR_INVALID_ARG, "the backward takes no kv_lengths");
-  if (nt_status st = window_operands(a)) return st;
-  const int ve = vec_elems(a.dtype);
-  const int64_t cq = (int64_t)a.heads * a.head_dim, ck = (int64_t)a.kv_heads * a.head_dim;
-  const int64_t nq = a.q_layout->sum_n, nk = a.kv_layout->sum_n;
-  if (nq > 0 && !a.lse) return nt::fail(NT_ERR_INVALID_ARG, "the backward needs the forward's lse");
-  if (nt_status st = matrix_operand(a.dout, a.ld_dout, cq, nq, ve, "dout")) return st;
-  if (nt_status st = matrix_operand(a.dq, a.ld_dq, cq, nq, ve, "dq")) return st;
-  if (nt_status st = matrix_operand(a.dk, a.ld_dk, ck, nk, ve, "dk")) return st;
-  if (nt_status st = matrix_operand(a.dv, a.ld_dv, ck, nk, ve, "dv")) return st;
-  for (const void* out : {(const void*)(nq ? a.dq : nullptr), (const void*)(nk ? a.dk : nullptr), (const void*)(nk ? a.dv : nullptr)})
-    if (out && (out == a.q || out == a.k || out == a.v || out == a.o || out == a.dout))
-      return nt::fail(NT_ERR_INVALID_ARG, "dq, dk and dv must not alias the operands");
-  if ((nk && a.dk == a.dv) || (nq && nk && (a.dq == a.dk || a.dq == a.dv)))
-    return nt::fail(NT_ERR_INVALID_ARG, "dq, dk and dv must not alias one another");
-  if (nq == 0 && nk == 0) return NT_OK;
+  if (nt_status st = window_operands(a, true)) return st;
+  if (a.q_layout->sum_n == 0 && a.kv_layout->sum_n == 0) return NT_OK;
   if (nt_status st = need_workspace(nt::window_backward_workspace_bytes(a), a.workspace, a.workspace_bytes,
                                     "nt_window_attention_backward_workspace"))
     return st;

@@ -161,3 +161,27 @@ def test_nothing_to_do_is_ok():
     assert embed_backward(rows=0, acc=1, ids=None, dy=None, ws=None, ws_bytes=0) == B.NT_OK
     a = window_args(q_layout=host([0, 0]), kv_layout=host([0, 0]))
     assert status("nt_window_attention", C.byref(a), None) == B.NT_ERR_INVALID_ARG      # host-only layout, checked first
+
+
+BACKWARD = [
+    (dict(kv_lengths=P), "takes no kv_lengths"), (dict(lse=None), "needs the forward's lse"),
+    (dict(dout=None), "dout is NULL"), (dict(dout=P + 8), "dout must be 16-byte"), (dict(ld_dout=120), "dout's row stride"),
+    (dict(dq=None), "dq is NULL"), (dict(dq=P + 8), "dq must be 16-byte"), (dict(ld_dq=127), "dq's row stride"),
+    (dict(dk=None), "dk is NULL"), (dict(dk=4 * P + 4), "dk must be 16-byte"), (dict(ld_dk=60), "dk's row stride"),
+    (dict(dv=None), "dv is NULL"), (dict(dv=5 * P + 2), "dv must be 16-byte"), (dict(ld_dv=68), "dv's row stride"),
+    (dict(dq=P), "must not alias the operands"), (dict(dk=2 * P), "must not alias the operands"),
+    (dict(dv=P), "must not alias the operands"), (dict(dk=3 * P), "must not alias one another"),
+    (dict(dv=3 * P), "must not alias one another"), (dict(dv=4 * P), "must not alias one another"),
+]
+
+
+@pytest.mark.parametrize("kw,words", BACKWARD)
+def test_window_backward_names_the_operand(kw, words):
+    """Every operand of the backward is looked at before the layouts' device."""
+    assert status("nt_window_attention_backward", C.byref(window_args(**kw)), None) == B.NT_ERR_INVALID_ARG
+    assert words in error()
+
+
+def test_window_forward_names_the_lengths():
+    assert status("nt_window_attention", C.byref(window_args(kv_lengths=P + 2)), None) == B.NT_ERR_INVALID_ARG
+    assert "kv_lengths" in error()
