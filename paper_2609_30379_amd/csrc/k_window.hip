@@ -475,6 +475,9 @@ struct WindowPlan {
 };
 
 // Key tiles of the blocks of `size` rows: all of them, and the most of one block.
+// With a window a block's keys begin `left` before its first query and end `right`
+// past its last; without a bound on the right (none given, or one that no query
+// needs) they end with the sample, which is at most N past the first query.
 void count_tiles(const nt_window_args& a, int shift, int kt, int64_t* total, int64_t* most) {
   const nt_layout &Lq = *a.q_layout, &Lk = *a.kv_layout;
   const int64_t G = a.heads / a.kv_heads, size = (int64_t)1 << shift;
@@ -483,7 +486,10 @@ void count_tiles(const nt_window_args& a, int shift, int kt, int64_t* total, int
     const int64_t rows = Lq.lengths[i] * G, m = Lk.lengths[i];
     if (rows == 0 || m == 0) continue;
     int64_t keys = m;
-    if (a.left >= 0 && a.right >= 0) keys = std::min(m, a.left + a.right + (size - 1) / G + 2 + (int64_t)a.sinks);
+    if (a.left >= 0) {
+      const int64_t past = a.right >= 0 ? a.right + (size - 1) / G + 2 : Lq.lengths[i];
+      keys = std::min(m, a.left + past + a.sinks);
+    }
     const int64_t tiles = (keys + kt - 1) / kt + (a.left >= 0 && a.sinks > 0 ? 1 : 0);
     *total += (rows + size - 1) / size * tiles;
     *most = std::max(*most, tiles);

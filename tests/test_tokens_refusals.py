@@ -185,3 +185,25 @@ def test_window_backward_names_the_operand(kw, words):
 def test_window_forward_names_the_lengths():
     assert status("nt_window_attention", C.byref(window_args(kv_lengths=P + 2)), None) == B.NT_ERR_INVALID_ARG
     assert "kv_lengths" in error()
+
+
+@pytest.mark.parametrize("n,m,left,right,sinks", [(1, 32000, 1023, 0, 0), (1, 32000, 1023, 1, 0), (1, 32000, 1023, 1, 4),
+                                                  (3, 32000, 500, 40, 2), (5, 30000, 900, 5, 0)])
+def test_a_window_past_the_last_query_keeps_the_plan_small(n, m, left, right, sinks):
+    """A bound `right` that no query needs (right >= N) leaves the window of `left`
+    keys: a few queries over a long cache are not cut, and need no partial sums."""
+    a = window_args(q_layout=host([n]), kv_layout=host([m]), heads=12, kv_heads=12, head_dim=64, left=left, right=right,
+                    sinks=sinks)
+    bytes_ = C.c_uint64(77)
+    assert status("nt_window_attention_workspace", C.byref(a), C.byref(bytes_)) == B.NT_OK
+    assert bytes_.value == 0
+
+
+def test_all_keys_of_a_long_cache_are_cut():
+    """The same without a window on the left: 500 tiles for one block of rows."""
+    bytes_ = C.c_uint64()
+    for left in (-1, 32000):
+        a = window_args(q_layout=host([1]), kv_layout=host([32000]), heads=12, kv_heads=12, head_dim=64, left=left, right=1,
+                        sinks=0)
+        assert status("nt_window_attention_workspace", C.byref(a), C.byref(bytes_)) == B.NT_OK
+        assert bytes_.value >= 2 * 12 * (64 + 2) * 4
