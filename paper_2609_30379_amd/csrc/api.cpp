@@ -389,8 +389,8 @@ nt_status nt_layernorm_linear(const nt_linear_args* a, void* stream) {
     if (!a->residual && a->x_dtype != a->dtype) return nt::fail(NT_ERR_INVALID_ARG, "SwiGLU residual = x needs x in the output dtype");
   }
   if (a->dtype == NT_F32 && !swiglu && a->c_in > 4096) return nt::fail(NT_ERR_UNSUPPORTED, "f32 path needs c_in <= 4096");
-  if (a->epilogue == NT_EPI_RESIDUAL && !a->residual) return nt::fail(NT_ERR_INVALID_ARG, "residual epilogue needs residual");
-  if (gated && (!a->residual || !a->gate)) return nt::fail(NT_ERR_INVALID_ARG, "gated residual epilogue needs residual and gate");
+  if (a->rows > 0 && a->epilogue == NT_EPI_RESIDUAL && !a->residual) return nt::fail(NT_ERR_INVALID_ARG, "residual epilogue needs residual");
+  if (a->rows > 0 && gated && (!a->residual || !a->gate)) return nt::fail(NT_ERR_INVALID_ARG, "gated residual epilogue needs residual and gate");
   if (gated && a->n_tail) return nt::fail(NT_ERR_UNSUPPORTED, "the gated residual epilogue has no tail output");
   if (!gated && a->gate) return nt::fail(NT_ERR_INVALID_ARG, "gate is only read by the gated residual epilogue");
   if (a->epilogue == NT_EPI_SIGMOID_GLU &&

@@ -301,3 +301,15 @@ def test_linear_backward_rejects_misaligned_parameters(lib):
         setattr(a, field, C.c_void_p(0x7004))
         st = lib.nt_layernorm_linear_backward(C.byref(a), None)
         assert st == B.NT_ERR_INVALID_ARG and b"aligned" in lib.nt_last_error(), field
+
+
+@pytest.mark.parametrize("epilogue", ["residual", "gated_residual"])
+def test_linear_of_no_rows_needs_no_residual(lib, epilogue):
+    """A tensor of no rows has no memory: its NULL residual (and gate) is refused only where there are rows."""
+    a = B.LinearArgs()
+    a.c_in = a.c_out = a.ldx = a.ldy = a.ld_residual = a.ld_gate = 64
+    a.dtype = a.x_dtype = B.NT_BF16
+    a.epilogue = B.EPILOGUES[epilogue]
+    assert lib.nt_layernorm_linear(C.byref(a), None) == B.NT_OK
+    a.rows, a.x, a.w, a.y = 4, 0x1000, 0x2000, 0x3000
+    assert lib.nt_layernorm_linear(C.byref(a), None) == B.NT_ERR_INVALID_ARG and b"needs residual" in lib.nt_last_error()
