@@ -593,7 +593,8 @@ nt_status nt_pair_row_attention_backward_workspace(const nt_layout* layout, int3
  * normalised rows and the recomputed hidden are rounded to bf16 as the
  * forward consumed them.  Weight gradients (dw, db, dgamma, dbeta, dw2, db2:
  * fp32, contiguous, NULL = not wanted) are accumulated (overwritten with
- * overwrite_weights); dx (x_dtype or fp32) is overwritten unless accumulate_dx.  Partial sums are reduced in a fixed
+ * overwrite_weights, with zeros where there are no rows); dx (x_dtype or fp32)
+ * is overwritten unless accumulate_dx.  Partial sums are reduced in a fixed
  * order: the result is deterministic.  Every pointer, the LayerNorm affine
  * and the bias included, must be 16-byte aligned.                            */
 typedef struct {

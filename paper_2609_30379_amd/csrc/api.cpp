@@ -458,7 +458,9 @@ nt_status nt_layernorm_linear_backward(const nt_linear_bwd_args* a, void* stream
     return nt::fail(NT_ERR_INVALID_ARG, "row strides too small");
   if (a->x_dtype == NT_F32 && !a->ln_gamma && a->ldx != a->c_in)
     return nt::fail(NT_ERR_UNSUPPORTED, "fp32 x without a LayerNorm must be contiguous");
-  if (a->rows == 0) return NT_OK;
+  if (a->rows == 0)                    // weight gradients that are overwritten become zero
+    return check_hip(nt::launch_linear_backward(*a, nullptr, static_cast<hipStream_t>(stream)),
+                     "nt_layernorm_linear_backward launch");
   if (!a->x || !a->w || !a->dy) return nt::fail(NT_ERR_INVALID_ARG, "x, w and dy must be non-NULL");
   if (!aligned16(a->x) || !aligned16(a->w) || !aligned16(a->dy) || (a->dx && !aligned16(a->dx)) ||
       (a->w2 && !aligned16(a->w2)) || (a->ln_gamma && !aligned16(a->ln_gamma)) ||

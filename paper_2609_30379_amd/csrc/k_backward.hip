@@ -1491,7 +1491,19 @@ size_t linear_backward_workspace_bytes(const nt_linear_bwd_args& a) {
 }
 
 hipError_t launch_linear_backward(const nt_linear_bwd_args& a, void* ws, hipStream_t s) {
-  if (a.rows == 0) return hipSuccess;
+  if (a.rows == 0) {                   // sums over no rows: nothing to add, or zeros
+    if (!a.overwrite_weights) return hipSuccess;
+    const bool swiglu = a.epilogue == NT_EPI_SWIGLU_RESIDUAL, ln = a.ln_gamma != nullptr;
+    const int64_t K = a.c_in, N = a.c_out, Nw = swiglu ? 2 * (int64_t)a.hidden : N;
+    auto clear = [&](float* out, int64_t n) {
+      if (out) reduce_partials_kernel<<<blocks_for(n), 256, 0, s>>>(nullptr, 0, 0, n, out, 0);
+    };
+    clear(a.dw, Nw * K);
+    clear(a.db, Nw);
+    if (ln) clear(a.dgamma, K), clear(a.dbeta, K);
+    if (swiglu) clear(a.dw2, N * a.hidden), clear(a.db2, N);
+    return hipGetLastError();
+  }
   size_t n = 0;
   return run_linear_backward(a, ws, &n, s, true);
 }

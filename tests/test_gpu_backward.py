@@ -380,3 +380,25 @@ def test_weighted_square_loss(B, level, xdt, dxdt, C, pad):
     check(host(dx), ref_g, dxdt, what + " dx")
     if pad:
         assert torch.isnan(dx_full[:, C:]).all(), what + ": padding written"
+
+
+@pytest.mark.parametrize("epilogue,ln,hidden", [("none", False, 0), ("gelu", True, 0), ("swiglu_residual", True, 64)])
+def test_linear_backward_of_no_rows(epilogue, ln, hidden):
+    """Weight gradients over no rows: zero where they are overwritten, as they were where they accumulate."""
+    import torch
+    from paper_2609_30379_amd import binding as B
+    K, N = 64, 64 if hidden else 96
+    Nw = 2 * hidden if hidden else N
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16, device="cuda")   # noqa: E731
+    f = lambda *s: torch.full(s, 3.0, device="cuda")                      # noqa: E731
+    for over in (True, False):
+        out = dict(dw=f(Nw, K), db=f(Nw))
+        if ln:
+            out.update(dgamma=f(K), dbeta=f(K))
+        if hidden:
+            out.update(dw2=f(N, hidden), db2=f(N))
+        B.nt_layernorm_linear_backward(bf(0, K), bf(Nw, K), bf(0, N), ln=(f(K), f(K)) if ln else None, bias=f(Nw),
+                                       epilogue=epilogue, w2=bf(N, hidden) if hidden else None, hidden=hidden, dx=bf(0, K),
+                                       overwrite_weights=over, **out)
+        for k, g in out.items():
+            assert bool((g == (0.0 if over else 3.0)).all()), (k, over)

@@ -105,3 +105,16 @@ def test_captured_step_replays_with_new_tokens():
         eager.step(ids)
         want = [host(eager.loss)] + [host(v) for v in eager.grads.values()]
         assert all(np.array_equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_batch_without_tokens_has_zero_gradients():
+    import torch
+    from paper_2609_30379_amd import blocks
+    H, K, d = 2, 1, 32
+    model = blocks.TokenModel([0, 0], synth.token_model_params(20, 2, H, K, d, 128), H, K, d, left=5, sinks=1)
+    for g in model.grads.values():
+        g.fill_(float("nan"))
+    loss, x, grads = model.step(torch.zeros((0,), dtype=torch.int64, device="cuda"))
+    assert x.shape == (0, H * d) and not host(loss).any()
+    for k, g in grads.items():
+        assert not host(g).any(), k
