@@ -604,6 +604,27 @@ def nt_layernorm_linear_backward(x, w, dy, ln=None, eps: float = 1e-5, bias=None
     return dx
 
 
+def layernorm_linear_backward_workspace_bytes(rows: int, c_in: int, c_out: int, ln: bool = True, epilogue: str = "none",
+                                              hidden: int = 0) -> int:
+    """Workspace bytes of an nt_layernorm_linear_backward call on bf16 rows of
+    these sizes that gives dx and every weight gradient (operands with their
+    natural strides)."""
+    a = LinearBwdArgs()
+    a.rows, a.c_in, a.c_out, a.hidden = int(rows), int(c_in), int(c_out), int(hidden)
+    a.ldx, a.ld_dy, a.ld_dx = a.c_in, a.c_out, a.c_in
+    a.x_dtype = a.dx_dtype = NT_BF16
+    a.epilogue = EPILOGUES[epilogue]
+    some = C.c_void_p(16)                         # the query looks at which operands there are, not at what they hold
+    a.x = a.w = a.bias = a.dy = a.dx = a.dw = a.db = some
+    if ln:
+        a.ln_gamma = a.ln_beta = a.dgamma = a.dbeta = some
+    if epilogue == "swiglu_residual":
+        a.w2 = a.dw2 = a.db2 = some
+    n = C.c_uint64()
+    _check(load().nt_layernorm_linear_backward_workspace(C.byref(a), C.byref(n)))
+    return int(n.value)
+
+
 def attention_backward_workspace_bytes(layout: NestedLayout, axis: int, heads: int, head_dim: int,
                                        dtype: str = "bf16") -> int:
     n = C.c_uint64()

@@ -439,25 +439,13 @@ class MechanismRun:
         need = [B.layernorm_linear_workspace_bytes(Sx * cells, Cp, Cp, w.dtype, epilogue="swiglu_residual",
                                                    hidden=F),
                 B.loss_workspace_bytes(lay)]
-        need += [self._bwd_ws(Sx * cells, Cp, Cp, True, "swiglu_residual", F),
-                 self._bwd_ws(Sx * S, Cp, Cx, False, "residual", 0),
-                 self._bwd_ws(Sx * S, Cx, Cp if self.sep else 2 * Cp, False, "none", 0)]
+        bwd = B.layernorm_linear_backward_workspace_bytes
+        need += [bwd(Sx * cells, Cp, Cp, True, "swiglu_residual", F),
+                 bwd(Sx * S, Cp, Cx, False, "residual"),
+                 bwd(Sx * S, Cx, Cp if self.sep else 2 * Cp, False)]
         if self.rect:
-            need.append(self._bwd_ws(Mr, Cx, Cp, False, "none", 0))
+            need.append(bwd(Mr, Cx, Cp, False))
         self.scratch = B.workspace_tensor(max(need), device)
-
-    @staticmethod
-    def _bwd_ws(rows, K, N, ln, epi, F):
-        import ctypes
-        a = B.LinearBwdArgs()
-        a.rows, a.c_in, a.c_out = int(rows), int(K), int(N)
-        a.ldx, a.ld_dy, a.ld_dx = K, N, K
-        a.x_dtype = a.dx_dtype = B.NT_BF16
-        a.ln_gamma = ctypes.c_void_p(16) if ln else None
-        a.epilogue, a.hidden = B.EPILOGUES[epi], int(F)
-        n = ctypes.c_uint64()
-        B._check(B.load().nt_layernorm_linear_backward_workspace(ctypes.byref(a), ctypes.byref(n)))
-        return int(n.value)
 
     def step(self):
         """Forward, loss and backward; returns (loss terms, xt, pt, grads)."""
@@ -564,34 +552,15 @@ class TokenModel:
         self.loss, self.weight = e(lay.batch, dt=f32), torch.ones(lay.batch, dtype=f32, device=device)
         self.dx, self.do, self.dh, self.dqkv = e(T, C), e(T, C), e(T, self.F), e(T, Q)
         self.grads = {k: torch.empty(v.shape, dtype=f32, device=device) for k, v in self.W.items()}
+        bwd = B.layernorm_linear_backward_workspace_bytes
         need = [B.layernorm_linear_workspace_bytes(T, C, Q), B.layernorm_linear_workspace_bytes(T, C, self.F, epilogue="gelu"),
                 B.loss_workspace_bytes(lay),
                 B.window_attention_workspace_bytes(lay, heads, head_dim, **self.window),
                 B.window_attention_backward_workspace_bytes(lay, heads, head_dim, **self.window),
                 B.embedding_backward_workspace_bytes(T, self.W["embed"].shape[0], C),
-                self._backward_bytes(T, self.F, C, False, "residual"), self._backward_bytes(T, C, self.F, True, "gelu"),
-                self._backward_bytes(T, C, C, False, "residual"), self._backward_bytes(T, C, Q, True, "none")]
+                bwd(T, self.F, C, False, "residual"), bwd(T, C, self.F, True, "gelu"), bwd(T, C, C, False, "residual"),
+                bwd(T, C, Q)]
         self.scratch = B.workspace_tensor(max(need), device)
-
-    @staticmethod
-    def _backward_bytes(rows, K, N, ln, epilogue):
-        """Workspace of a linear backward as step() calls it (the query looks at
-        which operands are there, not at what they hold)."""
-        import ctypes
-        a = B.LinearBwdArgs()
-        a.rows, a.c_in, a.c_out = rows, K, N
-        a.ldx, a.ld_dy, a.ld_dx = K, N, K
-        a.x_dtype = a.dx_dtype = B.NT_BF16
-        a.epilogue, a.overwrite_weights, a.accumulate_dx = B.EPILOGUES[epilogue], 1, int(ln)
-        some = ctypes.c_void_p(16)
-        a.x = a.w = a.dy = a.dx = a.dw = a.db = some
-        if ln:
-            a.ln_gamma = a.ln_beta = a.dgamma = a.dbeta = some
-        if epilogue == "gelu":
-            a.bias = some
-        n = ctypes.c_uint64()
-        B._check(B.load().nt_layernorm_linear_backward_workspace(ctypes.byref(a), ctypes.byref(n)))
-        return int(n.value)
 
     def _qkv(self, t):
         a, b = self.H * self.d, (self.H + self.K) * self.d

@@ -313,3 +313,20 @@ def test_linear_of_no_rows_needs_no_residual(lib, epilogue):
     assert lib.nt_layernorm_linear(C.byref(a), None) == B.NT_OK
     a.rows, a.x, a.w, a.y = 4, 0x1000, 0x2000, 0x3000
     assert lib.nt_layernorm_linear(C.byref(a), None) == B.NT_ERR_INVALID_ARG and b"needs residual" in lib.nt_last_error()
+
+
+@pytest.mark.parametrize("rows,k,n,ln,epilogue,hidden", [(5000, 128, 128, True, "swiglu_residual", 512), (7000, 64, 96, False, "residual", 0),
+                                                         (333, 512, 1024, True, "gelu", 0), (0, 64, 64, True, "none", 0)])
+def test_linear_backward_workspace_covers_its_calls(lib, rows, k, n, ln, epilogue, hidden):
+    """The query by sizes holds for the call with every gradient, and for one into an fp32 dx."""
+    got = B.layernorm_linear_backward_workspace_bytes(rows, k, n, ln, epilogue, hidden)
+    for dx_dtype in (B.NT_BF16, B.NT_F32):
+        a = B.LinearBwdArgs()
+        a.rows, a.c_in, a.c_out, a.hidden, a.epilogue = rows, k, n, hidden, B.EPILOGUES[epilogue]
+        a.ldx, a.ld_dy, a.ld_dx, a.x_dtype, a.dx_dtype = k, n, k, B.NT_BF16, dx_dtype
+        a.x = a.w = a.w2 = a.bias = a.dy = a.dx = a.dw = a.db = a.dw2 = a.db2 = 0x1000
+        if ln:
+            a.ln_gamma = a.ln_beta = a.dgamma = a.dbeta = 0x1000
+        need = C.c_uint64()
+        assert lib.nt_layernorm_linear_backward_workspace(C.byref(a), C.byref(need)) == B.NT_OK
+        assert need.value <= got and (dx_dtype != B.NT_BF16 or need.value == got)
