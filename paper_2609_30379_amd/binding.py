@@ -192,7 +192,7 @@ def _mat(t, name):
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     shape, stride = t.shape, t.stride()
-    if len(shape) != 2 or (shape[0] > 0 and shape[1] > 1 and stride[1] != 1):
+    if len(shape) != 2 or (shape[1] > 1 and stride[1] != 1):
         raise ValueError(f"{name} must be 2-D with contiguous rows")
     return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1]
 

@@ -330,3 +330,23 @@ def test_linear_backward_workspace_covers_its_calls(lib, rows, k, n, ln, epilogu
         need = C.c_uint64()
         assert lib.nt_layernorm_linear_backward_workspace(C.byref(a), C.byref(need)) == B.NT_OK
         assert need.value <= got and (dx_dtype != B.NT_BF16 or need.value == got)
+
+
+def test_matrices_need_contiguous_rows_whatever_their_length():
+    """Also of an operand without rows: a transposed view is refused before its first row appears."""
+    class Fake:
+        is_cuda = True
+
+        def __init__(self, shape, stride):
+            self.shape, self._stride = shape, stride
+
+        def stride(self):
+            return self._stride
+
+        def data_ptr(self):
+            return 4096
+
+    for rows in (0, 1, 5):
+        assert B._mat(Fake((rows, 8), (8, 1)), "x") == (4096, 8)
+        with pytest.raises(ValueError, match="contiguous rows"):
+            B._mat(Fake((rows, 8), (1, 5)), "x")
