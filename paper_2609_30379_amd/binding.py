@@ -707,7 +707,8 @@ def _window_args(q_layout, heads, head_dim, kv_layout, kv_heads, left, right, si
     a.heads, a.head_dim = int(heads), int(head_dim)
     a.kv_heads = a.heads if kv_heads is None else int(kv_heads)
     a.left, a.right, a.sinks = int(left), int(right), int(sinks)
-    a.scale = 1.0 / math.sqrt(head_dim) if scale is None else float(scale)
+    # a head_dim below 1 is the library's to refuse
+    a.scale = 1.0 / math.sqrt(max(1, head_dim)) if scale is None else float(scale)
     a.dtype = dtype
     return a
 

@@ -207,3 +207,11 @@ def test_all_keys_of_a_long_cache_are_cut():
                         sinks=0)
         assert status("nt_window_attention_workspace", C.byref(a), C.byref(bytes_)) == B.NT_OK
         assert bytes_.value >= 2 * 12 * (64 + 2) * 4
+
+
+@pytest.mark.parametrize("head_dim", [0, -8])
+def test_the_default_scale_leaves_a_bad_head_dim_to_the_library(head_dim):
+    lay = host([5])
+    a = B._window_args(lay, 4, head_dim, None, 2, -1, 0, 0, None, B.NT_BF16)
+    assert status("nt_window_attention", C.byref(a), None) == B.NT_ERR_INVALID_ARG and "head_dim" in error()
+    assert B._window_args(lay, 4, 64, None, 2, -1, 0, 0, None, B.NT_BF16).scale == 0.125
