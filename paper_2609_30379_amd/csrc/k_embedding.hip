@@ -105,8 +105,9 @@ embedding_kernel(const TT* __restrict__ table, int64_t ld_table, uint32_t vocab,
 // launches: the sort is short and latency-bound, the clearing long and bound by
 // bytes (30011 rows of 768 fp32 and 14999 tokens, one launch: 15.6 us, 5.9 TB/s;
 // 128011 rows of 2048 and 131072 tokens, four launches: 190 us, 5.5 TB/s).
-// The first's whole gradient is 53 us with the one launch and lookup, 73 through the
-// passes; past kSmall a range's pairs no longer fit LDS.
+// Past kSmall a range's pairs no longer fit LDS.  There, at 16384 tokens, the whole
+// gradient takes 28 us with the one launch and 37 through the passes (C = 64, 32000 ids),
+// 35 and 49 (768, 30000), 119 and 122 (1024, 128000), 26 and 27 (64, 300).
 constexpr int kSmall = 16384, kRanges = 128, kRangeBits = 8, kMaxBins = 512;
 
 struct SortParams {
@@ -558,20 +559,28 @@ embedding_join_kernel(SumParams p, TG* __restrict__ dtable, int64_t ld) {
   write_row(dtable, ld, id, piece * kVE, acc, p);
 }
 
-// Sorted rows per chunk: 32, and up to 128 where there are 2048 chunks or more all
-// the same; longer chunks leave fewer partial sums to add.  At most 65536 chunks,
-// so that one token's run over all rows stays a short list of them.
+// Sorted rows per chunk: short ones give few tokens enough workgroups, long ones
+// leave fewer partial sums to add.  Whole gradient in us, for C = 64 and 32000 ids, 768
+// and 30000, 1024 and 128000, 64 and 300: chunks of 32 and 64 rows at 32768 tokens
+// 41 : 49, 56 : 61, 138 : 137, 28 : 33; at 100000 57 : 62, 95 : 90, 214 : 216, 40 : 40; at
+// 160000 65 : 67, 136 : 130, 259 : 252, 50 : 45.  Chunks of 64 and 128 at 262144 tokens
+// 74 : 85, 179 : 170, 317 : 312, 56 : 58; at 524288 90 : 98, 301 : 289, 473 : 463, 76 : 70.
+// At most 65536 chunks, so that one token's run over all rows stays a short list of them.
+constexpr int64_t kChunk64Rows = 100000, kChunk128Rows = 500000;
 int chunk_of(int64_t rows) {
-  return rows < 1 << 17 ? 32 : rows < 1 << 18 ? 64 : (int)std::max<int64_t>(128, (rows + 65535) >> 16);
+  return rows < kChunk64Rows ? 32 : rows < kChunk128Rows ? 64 : (int)std::max<int64_t>(128, (rows + 65535) >> 16);
 }
-// Pairs per tile / 256: small tiles where few would leave the sort to a handful of
-// workgroups, large ones where every tile adds up the counts of many.
-int tile_iter(int64_t rows) { return rows <= 1 << 17 ? 4 : 16; }
+// Pairs per tile / 256: small tiles give few tokens enough workgroups, large ones
+// leave fewer counts to go through (small and large, C = 64, 32000 ids: 800000 tokens
+// 117 and 124 us, 1.5 million 160 and 158, 3 million 295 and 265, 12 million 1056 and 916;
+// 131000 tokens 58 and 76).
+constexpr int64_t kLargeTileRows = 1500000;
+int tile_iter(int64_t rows) { return rows < kLargeTileRows ? 4 : 16; }
 // From so many pairs on (98 tiles), the tiles' counts are summed by a launch of their
-// own (C = 64, 32000 ids, with and without it: 262144 tokens 99.5 and 96.5 us, 400000
-// 102 and 103, 524288 102 and 108, 4 million 357 and 438; 131072 tokens at C = 2048,
-// where the clearing decides, 595 and 590).
-constexpr int64_t kScanRows = 400000;
+// own (C = 64, 32000 ids, with and without it: 65536 tokens 53 and 47 us, 100000 57 and
+// 56, 131000 58 and 61, 200000 67 and 77, 524288 90 and 124; at C = 2048, 100000 tokens
+// 227 and 229).
+constexpr int64_t kScanRows = 100000;
 
 struct Plan {
   bool small;

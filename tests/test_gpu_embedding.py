@@ -151,3 +151,21 @@ def test_outputs_that_are_operands_are_refused():
         B.nt_embedding(t, ids, t)
     with pytest.raises(B.NtError):
         B.nt_embedding_backward(ids, t, t)
+
+
+@pytest.mark.parametrize("rows", [16384, 16385, 99999, 100000, 131072, 131073, 499999, 500001, 1499999, 1500001])
+@pytest.mark.parametrize("vocab", [3, 1000])
+def test_gradient_on_both_sides_of_each_plan(rows, vocab):
+    """Where chunks, tiles and the way their counts are summed change, and next to a
+    power of two.  Whole numbers: every partial sum is exact."""
+    import torch
+    from paper_2609_30379_amd import binding as B
+    r = np.random.default_rng(rows + vocab)
+    ids = r.integers(-1, vocab + 1, rows).astype(np.int32)
+    dy = r.integers(-2, 3, (rows, 8)).astype(np.float32)
+    g = torch.full((vocab, 8), float("nan"), device="cuda")
+    B.nt_embedding_backward(torch.tensor(ids, device="cuda"), torch.tensor(dy, device="cuda"), g)
+    ok = (ids >= 0) & (ids < vocab)
+    ref = np.stack([np.bincount(ids[ok], dy[ok, j].astype(np.float64), vocab) for j in range(8)], 1)
+    assert np.abs(ref).max() < 2 ** 24
+    assert np.array_equal(host(g), ref)

@@ -215,3 +215,15 @@ def test_the_default_scale_leaves_a_bad_head_dim_to_the_library(head_dim):
     a = B._window_args(lay, 4, head_dim, None, 2, -1, 0, 0, None, B.NT_BF16)
     assert status("nt_window_attention", C.byref(a), None) == B.NT_ERR_INVALID_ARG and "head_dim" in error()
     assert B._window_args(lay, 4, 64, None, 2, -1, 0, 0, None, B.NT_BF16).scale == 0.125
+
+
+def test_embedding_gradient_has_no_border_at_powers_of_two():
+    """Chunks and tiles change where both sides were measured, not next to a round
+    number of tokens: one token more never changes the workspace by a hundredth."""
+    def need(rows):
+        n = C.c_uint64()
+        assert status("nt_embedding_backward_workspace", rows, 30000, 64, C.byref(n)) == B.NT_OK
+        return n.value
+    for p in range(15, 24):
+        a, b, c = (need((1 << p) + x) for x in (-1, 0, 1))
+        assert abs(b - a) < 0.01 * a and abs(c - b) < 0.01 * b, p
