@@ -118,3 +118,10 @@ def test_a_batch_without_tokens_has_zero_gradients():
     assert x.shape == (0, H * d) and not host(loss).any()
     for k, g in grads.items():
         assert not host(g).any(), k
+
+
+def test_training_step_of_a_wide_batch():
+    """More than 128 blocks of rows and 256 of keys: the attention's kernels of large calls."""
+    lengths, H, d = [1000, 700, 520], 16, 64
+    assert sum((n + 127) // 128 for n in lengths) * H > 256
+    test_training_step(lengths, H, H, d, 256, 1, dict(left=128, right=0, sinks=3))

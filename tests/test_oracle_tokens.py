@@ -79,3 +79,33 @@ def test_embedding_and_gradient():
         step[at] = 0.5                                                           # linear in the table
         diff = ((T.embedding(table + step, ids, 2.0) - T.embedding(table - step, ids, 2.0)) * w).sum()
         assert abs(diff - g[at]) < 1e-12 and mag[at] >= abs(g[at])
+
+
+@pytest.mark.parametrize("left,right,sinks", [(-1, 0, 0), (2, 0, 1), (1, 2, 2), (-1, -1, 0)])
+def test_gradients_against_autograd(left, right, sinks):
+    """Dense float64 autograd of the definition, shared heads and fewer keys than queries included."""
+    torch = pytest.importorskip("torch")
+    n, m, H, K, d, rng = [6, 0, 9, 4], [6, 3, 14, 2], 6, 2, 8, RNG(5)
+    q, k, v, w = (rng.standard_normal((r, h * d)) for r, h in ((sum(n), H), (sum(m), K), (sum(m), K), (sum(n), H)))
+    Q, Kt, V = (torch.tensor(x, dtype=torch.float64, requires_grad=True) for x in (q, k, v))
+    a = b = 0
+    total = torch.zeros((), dtype=torch.float64)
+    for i in range(len(n)):
+        for t in range(n[i]):
+            p = m[i] - n[i] + t
+            js = [j for j in range(m[i]) if (right < 0 or j <= p + right) and (left < 0 or j >= p - left or j < sinks)]
+            for h in range(H):
+                if not js:
+                    continue
+                c, r = slice(h * d, h * d + d), slice(h // (H // K) * d, h // (H // K) * d + d)
+                rows = [b + j for j in js]
+                weight = torch.softmax(0.3 * (Kt[rows, r] @ Q[a + t, c]), 0)
+                total = total + (weight @ V[rows, r]) @ torch.tensor(w[a + t, c])
+        a, b = a + n[i], b + m[i]
+    total.backward()
+    kw = dict(left=left, right=right, sinks=sinks, scale=0.3)
+    o, lse, _ = T.window_attention(q, k, v, n, m, H, K, d, **kw)
+    assert abs((o * w).sum() - float(total)) < 1e-11
+    grads, _ = T.window_attention_backward(q, k, v, o, lse, w, n, m, H, K, d, **kw)
+    for g, x in zip(grads, (Q, Kt, V)):
+        assert np.allclose(g, x.grad.numpy(), rtol=0, atol=1e-11)
