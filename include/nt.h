@@ -662,7 +662,10 @@ nt_status nt_layernorm_linear_backward_workspace(const nt_linear_bwd_args* args,
  *            uses now, of the M_i slots it has (clamped to [0, M_i]); M_i above is
  *            this number then.  One layout serves a growing cache, and a captured
  *            graph follows the lengths.  Forward only.
- *   dtype    bf16 (matrix cores, fp32 softmax and sums) or f32.
+ *   dtype    f32 (fp32 throughout), or bf16: scores, softmax and every sum in
+ *            fp32; the weights exp(s_j - m) are rounded to bf16 before they
+ *            multiply v (their sum, and lse, are of the unrounded ones), and in
+ *            the backward P and dS before they multiply dout, k and q.
  *   head_dim a multiple of 8, at most 128.
  *   Row strides are multiples of 8 elements (bf16) or 4 (f32).
  * Workspace: nt_window_attention_workspace /
@@ -718,8 +721,10 @@ nt_status nt_window_attention_workspace(const nt_window_args* args, uint64_t* by
 /* Gradients of nt_window_attention (without kv_lengths):
  *   P = exp(s - lse), D = sum_c dout o, dS = P (dout v^T - D)
  *   dq = scale dS k,  dk = scale dS^T q,  dv = P^T dout
- * summed in fp32 without atomics (the same bits every time), rounded once;
- * a shared key/value head's gradient is the sum over its query heads.
+ * summed in fp32 without atomics (the same bits every time), the sums rounded
+ * once; bf16 calls round P and dS to bf16 before the products that use them
+ * (each off by at most 2^-8 of itself).
+ * A shared key/value head's gradient is the sum over its query heads.
  * Errors: as nt_window_attention, and NT_ERR_INVALID_ARG for kv_lengths.     */
 nt_status nt_window_attention_backward(const nt_window_args* args, void* stream);
 nt_status nt_window_attention_backward_workspace(const nt_window_args* args, uint64_t* bytes);
