@@ -104,7 +104,7 @@ embedding_kernel(const TT* __restrict__ table, int64_t ld_table, uint32_t vocab,
 // The gradient table is cleared meanwhile by further workgroups of the same
 // launches: the sort is short and latency-bound, the clearing long and bound by
 // bytes (30011 rows of 768 fp32 and 14999 tokens, one launch: 15.6 us, 5.9 TB/s;
-// 128011 rows of 2048 and 131072 tokens, four launches: 190 us, 5.5 TB/s).
+// 128011 rows of 2048 and 131072 tokens, six launches: 192 us, 5.5 TB/s).
 // Past kSmall a range's pairs no longer fit LDS.  There, at 16384 tokens, the whole
 // gradient takes 28 us with the one launch and 37 through the passes (C = 64, 32000 ids),
 // 35 and 49 (768, 30000), 119 and 122 (1024, 128000), 26 and 27 (64, 300).

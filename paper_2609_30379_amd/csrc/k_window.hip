@@ -112,12 +112,17 @@ __device__ __forceinline__ void write_out(const WindowParams& p, int64_t token, 
 // exponentials together: of a wave's time the matrix cores take 38 .. 40 % and the
 // vector instructions as much (no LDS bank conflicts), which two or three waves per
 // SIMD overlap in part; a wave in its products goes first (s_setprio), so that the
-// others' exponentials fill the time around them (causal window to 8192, 128
-// channels: 265 us without, 255 with).  Tiles of 32 keys at 128 channels cost 14 %,
-// four waves per SIMD at 64 channels a third (spills).
-//   64 samples of about 230 tokens, 12 heads of 64, left = right = 64: 39 us, 2.5 TB/s
-//   4 samples to 8192, 16 heads on 4 of 128, causal window of 1024: 239 us, 716 TFLOP/s
-//   two chunks of 300 .. 700 tokens over 8000 .. 30000, 16 heads on 4 of 64: 102 us, 590
+// others' exponentials fill the time around them (without and with, in turn: causal
+// window to 8192, 128 channels, 233 and 229 us; chunk over 30000 107 and 104; the
+// encoder's window the same).  Tiles of 32 keys at 128 channels cost 14 %, four waves
+// per SIMD at 64 channels a third (spills).  Each fragment read from LDS feeds one
+// product, 1.75 LDS instructions a product; more rows per wave is not tried.  155
+// registers at 64 channels and 253 at 128, no spills.  A call among many, on two cards:
+//   64 samples of about 230 tokens, 12 heads of 64, left = right = 64: 41 us, 2.4 TB/s
+//   4 samples to 8192, 16 heads on 4 of 128, causal window of 1024: 233 .. 247 us, 694 ..
+//   734 TFLOP/s
+//   two chunks of 300 .. 700 tokens over 8000 .. 30000, 16 heads on 4 of 64, the join of
+//   their splits included: 103 .. 108 us, 555 .. 580 TFLOP/s
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, DP == 128 ? (sizeof(T) == 4 ? 1 : 2) : DP == 64 && sizeof(T) == 4 ? 2 : 3)
 window_rows_kernel(WindowParams p) {
@@ -292,7 +297,8 @@ window_rows_kernel(WindowParams p) {
 // so no wave waits for another before the end, where the four running sums are
 // joined through LDS.  Bound by the cache's bytes: a wave keeps a whole tile in
 // flight while it works on the one before, eight waves per compute unit together
-// 256 KB.  64 tokens over 500 .. 32000 keys, 32 heads on 8 of 128: 759 us, 5.0 TB/s
+// 256 KB; that takes all 256 registers, of bf16 at 64 channels 6 and at 128 channels 30
+// are spilled and read back in the tile loop.  64 tokens over 500 .. 32000 keys, 32 heads on 8 of 128: 759 us, 5.0 TB/s
 // (a large copy reaches 4.7 here, a large read alone 4.0); one token over a window
 // of 1023 keys, 12 heads of 64: 10 us, the latency of four dependent tiles and the
 // launch.  Eight waves per workgroup: 9 us for that token, 794 .. 815 for the 64.

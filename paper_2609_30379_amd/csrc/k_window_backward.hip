@@ -88,10 +88,11 @@ __device__ __forceinline__ void write_row(const WindowBwdParams& p, int64_t toke
 // dQ of 128 rows, 32 per wave: S^T = K Q^T, dP^T = V dO^T and dQ^T += K^T dS^T of one
 // tile of keys after another, the tiles twice in LDS as in the forward; dP starts from
 // -D, which saves the subtraction.  Q and dO stay in registers, so past 64 channels
-// tiles of 64 keys spill; of 32 they do not, and both K and V of the next tile can be
-// on their way at once (N to 8192, 16 heads on 4 of 128: 427 us in tiles of 64, 369 ..
-// 388 in tiles of 32, about 790 TFLOP/s).  Bound as the forward is: matrix cores 38 %,
-// vector instructions 27 % of the time.  64 channels, N 200 .. 1024: 27 us.
+// bf16 tiles of 64 keys spill 31 registers; tiles of 32 spill 10, some of them read back
+// in the loop, and both K and V of the next tile can be on their way at once (N to 8192,
+// 16 heads on 4 of 128, the whole training step: 1301 us in tiles of 64, 1260 in tiles
+// of 32; dQ 351 .. 424, median 372, 790 TFLOP/s).  Bound as the forward is: matrix cores
+// 38 %, vector instructions 27 % of the time.  64 channels, N 200 .. 1024: 27 us.
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, DP == 32 ? 3 : DP == 128 && sizeof(T) == 4 ? 1 : 2)
 window_dq_kernel(WindowBwdParams p) {
@@ -482,13 +483,14 @@ template <typename T, int DP, int RT, int THREADS> struct RowTile {
 
 // dK and dV of 128 keys, 32 per wave; the workgroup walks the rows that see them, 64
 // (fp32: 32) at a time through one tile of q and dout in LDS while the next is on its
-// way in registers.  K, V and both gradients of a wave's keys are 320 registers at 128
-// channels, so one wave per SIMD; two waves, forced, spill (1130 us for N to 8192, 16
-// heads on 4 of 128, against 800), and dK and dV in workgroups of their own
-// compute S twice (907).  Bound by the products' latency with nothing else to issue:
-// matrix cores 33 % of the time it runs.  The 428 workgroups on 256 compute units
-// would take two turns, so their rows are cut in four parts: 761 .. 800 -> 679 us, 580
-// TFLOP/s, and 47 in the join.  Without any new rows to read it takes 9 % less;
+// way in registers.  K, V and both gradients of a wave's keys are 192 registers at 128
+// bf16 channels, and 371 of 512 are used, so one wave per SIMD; two waves, forced, spill
+// (1130 us for N to 8192, 16 heads on 4 of 128, against 800 then), and dK and dV in
+// workgroups of their own compute S twice (907).  fp32 past 64 channels uses all 512 and
+// spills 24.  Bound by the products' latency with nothing else to issue: matrix cores
+// 33 % of the time it runs.  The 428 workgroups on 256 compute units would take two
+// turns, so their rows are cut in four parts: 761 .. 800 us uncut, now 621 .. 756, median
+// 660, 595 TFLOP/s, and 46 in the join.  Without any new rows to read it takes 9 % less;
 // workgroups that walk shared rows at the same time gain nothing.
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, DP == 128 || (DP == 64 && sizeof(T) == 4) ? 1 : 2)
@@ -612,7 +614,8 @@ key_join_kernel(WindowBwdParams p) {
 //   (every row sees every sink there) and leaves its sums for sink_sum_kernel.
 // Bound by latency, four walks instead of one: 13 us for fp32, N 66 .. 317, 4 heads of
 // 32 (31 in blocks of 128 keys); 28 for N 200 .. 1024, 8 heads on 2 of 64 (54); the
-// sinks of N to 8192, 16 heads on 4 of 128: 22.
+// sinks of N to 8192, 16 heads on 4 of 128: 23.  fp32 past 64 channels spills: 121
+// registers here, stored and read back in the loop, and 38 in the dQ of few rows.
 template <typename T, int DP, bool SINKS>
 __global__ void __launch_bounds__(256, sizeof(T) == 4 || DP == 128 ? 1 : 2)
 window_dkv_few_kernel(WindowBwdParams p) {
